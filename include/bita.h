@@ -52,8 +52,13 @@ extern "C" {
 #define BITA_ERR_UNSUPPORTED -4   /* shape outside what the kernels are built for             */
 #define BITA_ERR_HIP         -5   /* a HIP runtime call failed; see bita_last_error()         */
 
+/* types of the tensors of the 8-bit linear layers (everywhere else a tensor's type is fixed) */
+#define BITA_F32  0
+#define BITA_BF16 1
+
 #define BITA_MAX_ROWS   512      /* R limit of one template                                   */
 #define BITA_MAX_TOPK    64      /* kmax limit                                                */
+#define BITA_Q8_MAX_K 131071     /* longest row of 8-bit integers: sums of 128 * 128 * K stay within 32 bits */
 
 /* Decoder shape.  LLaMA-2 architecture (the paper's base models, Sec. 4.1.2):
  * RMSNorm, rotary embeddings in the half-split pairing (i, i + head_dim/2),
@@ -316,6 +321,46 @@ size_t bita_gemm_noalloc_max_scratch_bytes(void);
 size_t bita_gemm_noalloc_scratch_bytes(int32_t m_rows, int64_t n_rows, int64_t k);
 int bita_gemm_noalloc(const void *d_a, const void *d_a_lo, int32_t m_rows, int64_t k, int64_t lda,
                       const void *d_w_packed, int64_t n_rows, float *d_out, void *stream);
+
+/* ---- 8-bit linear layers -----------------------------------------------------------------
+ * Weights and activations as signed 8-bit integers with an fp32 scale per row (channel, token): half the weight
+ * bytes of bf16.  A row v is held as q_i = round(127 v_i / a), ties to even, and s = a / 127 with a = max |v_i|, so
+ * that v_i is q_i s within half a step; a row of zeros has q = 0, s = 0, and a row with a NaN or an infinity q = 0,
+ * s = NaN (whatever it is multiplied with is NaN).  Every q is the exactly rounded one (bita_silu_mul_q8: rounded from double).
+ * x_type, delta_type, out_type: BITA_F32 or BITA_BF16.  ld*: elements from one row to the next; any alignment and any
+ * k is accepted, and rows whose start and stride are multiples of 16 bytes are the fast ones.  The outputs of the three
+ * row calls do not overlap their inputs, except where stated.
+ *
+ * bita_quantize_rows  rows as they are: an attention output in front of its projection; a weight [N][K], one scale a channel.
+ *                     1 <= k <= BITA_Q8_MAX_K
+ * bita_norm_q8        h = x + delta (delta optional; added in fp32, rounded to x's type, stored in d_total, which may be
+ *                     d_x with its stride), v = h / sqrt(mean(h^2) + eps) * gain, d_gain bf16 [d].  1 <= d <= 16384
+ * bita_silu_mul_q8    v = silu(gate) * up of a gate/up product [M][2 d_ffn]: tile 16 = tiles of 16 gate columns, each followed
+ *                     by its 16 up columns (bita_pack_weight's interleaving; d_ffn a multiple of 16), tile 0 = all gate columns
+ *                     first.  1 <= d_ffn <= BITA_Q8_MAX_K
+ * All three only enqueue one kernel on `stream`. */
+int bita_quantize_rows(const void *d_x, int32_t x_type, int32_t m_rows, int64_t k, int64_t ldx, int8_t *d_q, int64_t ldq,
+                       float *d_scale, void *stream);
+int bita_norm_q8(const void *d_x, int32_t x_type, int32_t m_rows, int64_t d, int64_t ldx, const void *d_delta, int32_t delta_type,
+                 int64_t ld_delta, const void *d_gain, float eps, void *d_total, int64_t ld_total, int8_t *d_q, int64_t ldq,
+                 float *d_scale, void *stream);
+int bita_silu_mul_q8(const void *d_gate_up, int32_t x_type, int32_t m_rows, int64_t d_ffn, int64_t ldx, int32_t tile, int8_t *d_q,
+                     int64_t ldq, float *d_scale, void *stream);
+
+/* The packed form of an 8-bit weight [N][K]: 1 KiB blocks, each one MFMA operand (16 rows x 64 k), ordered
+ * [pair of k-steps][16-row tile][k-step of the pair]; K is padded with zeros to a multiple of 128, N to one of 16.
+ * Arguments as bita_pack_weight's, but for d_src: signed 8-bit integers, `ld` apart (any k and alignment; n_rows a multiple of
+ * 16 unless the source's last tile is the destination's last).  d_dst holds bita_packed_q8_bytes(dst_total_rows, k). */
+size_t bita_packed_q8_bytes(int64_t n_rows, int64_t k);
+int bita_pack_weight_q8(const int8_t *d_src, int64_t n_rows, int64_t k, int64_t ld, void *d_dst, int64_t dst_total_rows,
+                        int64_t dst_tile0, int64_t dst_tile_stride, void *stream);
+
+/* d_out[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n]: the sums are 32-bit integers and exact, each multiplied
+ * in fp32 by the row's scale, then by the channel's, and rounded once more where out_type is BITA_BF16.
+ *   d_a [m_rows][lda] 8-bit integers, as the row calls leave them: d_a and lda multiples of 16, lda >= k.  Columns from k to the
+ *   next multiple of 16 may hold anything, and are read (of the last row too).  d_w_scale is in the order of the packed rows.  1 <= k <= BITA_Q8_MAX_K; any m_rows, n_rows. */
+int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t m_rows, int64_t k, const void *d_w_packed,
+                 const float *d_w_scale, int64_t n_rows, void *d_out, int32_t out_type, int64_t ldo, void *stream);
 
 /* Measurement aid: while enabled, bita_verify_step brackets each of its GEMM launches with
  * a pair of HIP events on the caller's stream (not usable under graph capture).

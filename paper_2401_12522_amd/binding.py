@@ -19,6 +19,7 @@ EXPORTS = [
     "bita_gemm_workspace_bytes", "bita_gemm", "bita_gemm_noalloc_max_scratch_bytes", "bita_gemm_noalloc_scratch_bytes",
     "bita_gemm_noalloc", "bita_select", "bita_tune_gemm", "bita_gemm_plan_info", "bita_gemm_plan_detail", "bita_profile_enable",
     "bita_profile_disable", "bita_profile_read", "bita_last_error",
+    "bita_quantize_rows", "bita_norm_q8", "bita_silu_mul_q8", "bita_packed_q8_bytes", "bita_pack_weight_q8", "bita_gemm_q8",
 ]
 
 
@@ -104,6 +105,13 @@ def lib():
     L.bita_profile_disable.restype, L.bita_profile_disable.argtypes = None, []
     L.bita_profile_read.restype, L.bita_profile_read.argtypes = C.c_int, [i32, vp, vp, vp]
     L.bita_last_error.restype, L.bita_last_error.argtypes = C.c_char_p, []
+    L.bita_quantize_rows.restype, L.bita_quantize_rows.argtypes = C.c_int, [vp, i32, i32, i64, i64, vp, i64, vp, vp]
+    L.bita_norm_q8.restype = C.c_int
+    L.bita_norm_q8.argtypes = [vp, i32, i32, i64, i64, vp, i32, i64, vp, C.c_float, vp, i64, vp, i64, vp, vp]
+    L.bita_silu_mul_q8.restype, L.bita_silu_mul_q8.argtypes = C.c_int, [vp, i32, i32, i64, i64, i32, vp, i64, vp, vp]
+    L.bita_packed_q8_bytes.restype, L.bita_packed_q8_bytes.argtypes = sz, [i64, i64]
+    L.bita_pack_weight_q8.restype, L.bita_pack_weight_q8.argtypes = C.c_int, [vp, i64, i64, i64, vp, i64, i64, i64, vp]
+    L.bita_gemm_q8.restype, L.bita_gemm_q8.argtypes = C.c_int, [vp, i64, vp, i32, i64, vp, vp, i64, vp, i32, i64, vp]
     _lib = L
     return L
 
@@ -497,3 +505,133 @@ def tree_attention(tmpl, q, k_cache, v_cache, k_tree, v_tree, prompt_k, prompt_v
                                      _ptr(k_tree_lo), _ptr(v_tree_lo), _ptr(prompt_k), _ptr(prompt_v), _ptr(ctx_len), B, Hq, Hkv, hd, P, smax,
                                      int(ctx_hint), _ptr(ws), ws.numel(), _ptr(out), _ptr(out_lo), _stream()))
     return (out, out_lo) if two_plane_out else out
+
+
+# ---- 8-bit linear layers ---------------------------------------------------------------------------------------------
+_F32_BF16 = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _matrix(name, t, types, rows=None, cols=None):
+    """t is a cuda matrix of one of these types and this size whose rows have neighbouring elements; its row stride."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in types):
+        raise ValueError(f"{name}: a cuda matrix of {' or '.join(str(x) for x in types)} is wanted")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols) or t.shape[0] < 1 or t.shape[1] < 1:
+        raise ValueError(f"{name}: {tuple(t.shape)}, wanted {rows if rows is not None else 'any'} x {cols if cols is not None else 'any'}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row have to be neighbours")
+    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if ld < t.shape[1]:
+        raise ValueError(f"{name}: rows overlap (stride {ld})")
+    return ld
+
+
+def _vector(name, t, n, dtype):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 1 and t.shape[0] == n and t.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous cuda vector of {n} {dtype} is wanted")
+
+
+def _same_device(*ts):
+    dev = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def empty_q8(rows, cols, device="cuda"):
+    """An int8 matrix whose rows are a multiple of 16 bytes apart, as gemm_q8 reads them."""
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
+
+
+def _q8_out(x, rows, cols, q, scale):
+    if q is None:
+        q = empty_q8(rows, cols, x.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    ldq = _matrix("q", q, (torch.int8,), rows, cols)
+    _vector("scale", scale, rows, torch.float32)
+    return q, scale, ldq
+
+
+def quantize_rows(x, q=None, scale=None):
+    """x: cuda [M][K], float32 or bfloat16.  Every row as 8-bit integers and a scale: (q int8 [M][K], scale fp32 [M]), written into
+    q and scale where they are given."""
+    ldx = _matrix("x", x, tuple(_F32_BF16))
+    m, k = x.shape
+    q, scale, ldq = _q8_out(x, m, k, q, scale)
+    _same_device(x, q, scale)
+    _check(lib().bita_quantize_rows(_ptr(x), _F32_BF16[x.dtype], m, k, ldx, _ptr(q), ldq, _ptr(scale), _stream()))
+    return q, scale
+
+
+def norm_q8(x, gain, eps, delta=None, total=None, q=None, scale=None):
+    """RMSNorm of x + delta times gain (bfloat16 [D]), rows as 8-bit integers: (q, scale).  x, delta: cuda [M][D], float32 or
+    bfloat16.  With delta, x + delta is stored in total (x's type and size); total None: in x itself."""
+    ldx = _matrix("x", x, tuple(_F32_BF16))
+    m, d = x.shape
+    _vector("gain", gain, d, torch.bfloat16)
+    ldd = ldt = 0
+    if delta is not None:
+        ldd = _matrix("delta", delta, tuple(_F32_BF16), m, d)
+        total = x if total is None else total
+        ldt = _matrix("total", total, (x.dtype,), m, d)
+    elif total is not None:
+        raise ValueError("total: there is nothing to store without delta")
+    q, scale, ldq = _q8_out(x, m, d, q, scale)
+    _same_device(x, gain, delta, total, q, scale)
+    _check(lib().bita_norm_q8(_ptr(x), _F32_BF16[x.dtype], m, d, ldx, _ptr(delta), 0 if delta is None else _F32_BF16[delta.dtype], ldd, _ptr(gain),
+                              float(eps), _ptr(total), ldt, _ptr(q), ldq, _ptr(scale), _stream()))
+    return q, scale
+
+
+def silu_mul_q8(gate_up, tile=0, q=None, scale=None):
+    """silu(gate) * up of gate_up, cuda [M][2F], float32 or bfloat16, rows as 8-bit integers: (q int8 [M][F], scale).  tile 16: tiles of
+    16 gate columns, each followed by its 16 up columns, as a product with an interleaved weight leaves them; tile 0: all gate columns first."""
+    ldx = _matrix("gate_up", gate_up, tuple(_F32_BF16))
+    m, f = gate_up.shape[0], gate_up.shape[1] // 2
+    if gate_up.shape[1] % 2 or not f:
+        raise ValueError(f"gate_up: {gate_up.shape[1]} columns are not two halves")
+    q, scale, ldq = _q8_out(gate_up, m, f, q, scale)
+    _same_device(gate_up, q, scale)
+    _check(lib().bita_silu_mul_q8(_ptr(gate_up), _F32_BF16[gate_up.dtype], m, f, ldx, int(tile), _ptr(q), ldq, _ptr(scale), _stream()))
+    return q, scale
+
+
+def packed_q8_bytes(n_rows, k):
+    return lib().bita_packed_q8_bytes(n_rows, k)
+
+
+def pack_weight_q8(src, dst=None, tile0=0, tile_stride=1, total_rows=None):
+    """src: int8 cuda [N][K] (quantize_rows of a weight).  Returns the packed uint8 buffer (allocated here when dst is None,
+    sized for total_rows rows)."""
+    ld = _matrix("src", src, (torch.int8,))
+    n, k = src.shape
+    total_rows = total_rows or n
+    need = packed_q8_bytes(total_rows, k)
+    if dst is None:
+        dst = torch.empty(need, dtype=torch.uint8, device=src.device)
+    elif not (dst.is_cuda and dst.dtype == torch.uint8 and dst.is_contiguous() and dst.numel() >= need):
+        raise ValueError(f"dst: a contiguous cuda buffer of {need} uint8 is wanted")
+    _same_device(src, dst)
+    _check(lib().bita_pack_weight_q8(_ptr(src), n, k, ld, _ptr(dst), total_rows, tile0, tile_stride, _stream()))
+    return dst
+
+
+def gemm_q8(a, a_scale, w_packed, w_scale, n_rows, out=None, out_dtype=torch.float32):
+    """a: int8 cuda [M][K] with its rows' scales (quantize_rows, norm_q8, silu_mul_q8); w_packed: pack_weight_q8 of an int8 [n_rows][K],
+    w_scale its rows' scales in packed order.  Returns [M][n_rows] in float32 or bfloat16, written into out where it is given."""
+    lda = _matrix("a", a, (torch.int8,))
+    m, k = a.shape
+    if m == 1:
+        lda = (lda + 15) // 16 * 16
+    if lda % 16 or a.data_ptr() % 16 or a.untyped_storage().nbytes() - a.storage_offset() < (m - 1) * lda + (k + 15) // 16 * 16:
+        raise ValueError("a: rows have to start at multiples of 16 bytes and to be readable to the next one behind their end (empty_q8)")
+    _vector("a_scale", a_scale, m, torch.float32)
+    _vector("w_scale", w_scale, n_rows, torch.float32)
+    if not (w_packed.is_cuda and w_packed.dtype == torch.uint8 and w_packed.is_contiguous() and w_packed.numel() >= packed_q8_bytes(n_rows, k)):
+        raise ValueError(f"w_packed: a contiguous cuda buffer of {packed_q8_bytes(n_rows, k)} uint8 is wanted")
+    if out is None:
+        out = torch.empty((m, n_rows), dtype=out_dtype, device=a.device)
+    ldo = _matrix("out", out, tuple(_F32_BF16), m, n_rows)
+    _same_device(a, a_scale, w_packed, w_scale, out)
+    _check(lib().bita_gemm_q8(_ptr(a), lda, _ptr(a_scale), m, k, _ptr(w_packed), _ptr(w_scale), n_rows, _ptr(out), _F32_BF16[out.dtype], ldo, _stream()))
+    return out

@@ -1,0 +1,55 @@
+"""What the 8-bit linear layers refuse, before any device call (CPU only)."""
+import pytest
+
+P = 1 << 20        # a pointer that is never followed: multiple of 16
+F32, BF16 = 0, 1
+
+
+def _lib():
+    from paper_2401_12522_amd import binding
+    return binding.lib()
+
+
+def _call(name, good, **bad):
+    args = dict(good, **bad)
+    return getattr(_lib(), name)(*args.values())
+
+
+ROWS = dict(x=P, x_type=F32, m=4, k=64, ldx=64, q=P, ldq=64, scale=P, stream=None)
+NORM = dict(x=P, x_type=F32, m=4, d=64, ldx=64, delta=P, delta_type=BF16, ld_delta=64, gain=P, eps=1e-5, total=P, ld_total=64, q=P, ldq=64,
+            scale=P, stream=None)
+GATE = dict(x=P, x_type=BF16, m=4, f=64, ldx=128, tile=16, q=P, ldq=64, scale=P, stream=None)
+PACK = dict(src=P, n=32, k=64, ld=64, dst=P, total=64, tile0=0, stride=1, stream=None)
+GEMM = dict(a=P, lda=64, a_scale=P, m=4, k=64, w=P, w_scale=P, n=64, out=P, out_type=F32, ldo=64, stream=None)
+
+
+@pytest.mark.parametrize("name,good,bad,code", [
+    ("bita_quantize_rows", ROWS, dict(x=None), -1), ("bita_quantize_rows", ROWS, dict(q=None), -1), ("bita_quantize_rows", ROWS, dict(scale=None), -1),
+    ("bita_quantize_rows", ROWS, dict(x_type=2), -1), ("bita_quantize_rows", ROWS, dict(m=0), -1), ("bita_quantize_rows", ROWS, dict(k=0), -1),
+    ("bita_quantize_rows", ROWS, dict(ldx=63), -1), ("bita_quantize_rows", ROWS, dict(ldq=63), -1),
+    ("bita_quantize_rows", ROWS, dict(k=131072, ldx=131072, ldq=131072), -4),
+    ("bita_norm_q8", NORM, dict(x=None), -1), ("bita_norm_q8", NORM, dict(gain=None), -1), ("bita_norm_q8", NORM, dict(total=None), -1),
+    ("bita_norm_q8", NORM, dict(delta_type=7), -1), ("bita_norm_q8", NORM, dict(ld_delta=60), -1), ("bita_norm_q8", NORM, dict(ld_total=60), -1),
+    ("bita_norm_q8", NORM, dict(ld_total=80), -1), ("bita_norm_q8", NORM, dict(eps=-1.0), -1), ("bita_norm_q8", NORM, dict(eps=float("nan")), -1),
+    ("bita_norm_q8", NORM, dict(d=16385, ldx=16400, ld_delta=16400, ld_total=16400, ldq=16400), -4), ("bita_norm_q8", NORM, dict(m=-1), -1),
+    ("bita_silu_mul_q8", GATE, dict(x=None), -1), ("bita_silu_mul_q8", GATE, dict(ldx=127), -1), ("bita_silu_mul_q8", GATE, dict(tile=8), -1),
+    ("bita_silu_mul_q8", GATE, dict(f=40), -1), ("bita_silu_mul_q8", GATE, dict(f=131088, ldx=1 << 20, ldq=1 << 20), -4),
+    ("bita_pack_weight_q8", PACK, dict(src=None), -1), ("bita_pack_weight_q8", PACK, dict(dst=P + 8), -1), ("bita_pack_weight_q8", PACK, dict(ld=63), -1),
+    ("bita_pack_weight_q8", PACK, dict(tile0=3), -1), ("bita_pack_weight_q8", PACK, dict(stride=4), -1), ("bita_pack_weight_q8", PACK, dict(stride=0), -1),
+    ("bita_pack_weight_q8", PACK, dict(n=20), -4), ("bita_pack_weight_q8", PACK, dict(k=131072, ld=131072), -4),
+    ("bita_gemm_q8", GEMM, dict(a=None), -1), ("bita_gemm_q8", GEMM, dict(a_scale=None), -1), ("bita_gemm_q8", GEMM, dict(w=None), -1),
+    ("bita_gemm_q8", GEMM, dict(w_scale=None), -1), ("bita_gemm_q8", GEMM, dict(out=None), -1), ("bita_gemm_q8", GEMM, dict(m=0), -1),
+    ("bita_gemm_q8", GEMM, dict(n=0), -1), ("bita_gemm_q8", GEMM, dict(k=0), -1), ("bita_gemm_q8", GEMM, dict(out_type=3), -1),
+    ("bita_gemm_q8", GEMM, dict(ldo=63), -1), ("bita_gemm_q8", GEMM, dict(lda=72), -1), ("bita_gemm_q8", GEMM, dict(lda=48), -1),
+    ("bita_gemm_q8", GEMM, dict(a=P + 8), -1), ("bita_gemm_q8", GEMM, dict(k=131072, lda=131088), -4),
+])
+def test_refused_with_a_message(name, good, bad, code):
+    assert _call(name, good, **bad) == code
+    assert name.encode() in _lib().bita_last_error()
+
+
+def test_packed_sizes():
+    L = _lib()
+    assert L.bita_packed_q8_bytes(32, 688) == 2 * 6 * 2048
+    assert L.bita_packed_q8_bytes(33, 1) == 3 * 2048
+    assert L.bita_packed_q8_bytes(0, 5) == L.bita_packed_q8_bytes(5, 0) == 0
