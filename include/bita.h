@@ -58,6 +58,7 @@ extern "C" {
 
 #define BITA_MAX_ROWS   512      /* R limit of one template                                   */
 #define BITA_MAX_TOPK    64      /* kmax limit                                                */
+#define BITA_Q8_MAX_LD (1 << 23) /* largest row stride of bita_gemm_q8's activations, bytes             */
 #define BITA_Q8_MAX_K 131071     /* longest row of 8-bit integers: sums of 128 * 128 * K stay within 32 bits */
 
 /* Decoder shape.  LLaMA-2 architecture (the paper's base models, Sec. 4.1.2):
@@ -357,10 +358,17 @@ int bita_pack_weight_q8(const int8_t *d_src, int64_t n_rows, int64_t k, int64_t 
 
 /* d_out[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n]: the sums are 32-bit integers and exact, each multiplied
  * in fp32 by the row's scale, then by the channel's, and rounded once more where out_type is BITA_BF16.
- *   d_a [m_rows][lda] 8-bit integers, as the row calls leave them: d_a and lda multiples of 16, lda >= k.  Columns from k to the
- *   next multiple of 16 may hold anything, and are read (of the last row too).  d_w_scale is in the order of the packed rows.  1 <= k <= BITA_Q8_MAX_K; any m_rows, n_rows. */
+ *   d_a [m_rows][lda] 8-bit integers, as the row calls leave them: d_a and lda multiples of 16, k <= lda <= BITA_Q8_MAX_LD.  Columns
+ *   from k to the next multiple of 16 may hold anything, and are read (of the last row too).  d_w_scale is in the order of the packed
+ *   rows.  1 <= k <= BITA_Q8_MAX_K; any m_rows, n_rows, ldo >= n_rows and alignment of d_out.
+ * d_ws: bita_gemm_q8_workspace_bytes() bytes of scratch at a multiple of 16 (the sums of a launch whose k is split; 0 bytes where it is not, and
+ * d_ws may then be NULL); nothing in it is kept from call to call.  One kernel, or two where k is split.
+ * bita_gemm_q8_plan_info: how a product of these sizes is cut (for tests and reports): out4 (HOST) = {rows and columns of a workgroup, k splits,
+ * 1 for the kernel of few rows, 0 for tiles of many}. */
+size_t bita_gemm_q8_workspace_bytes(int32_t m_rows, int64_t n_rows, int64_t k);
+int bita_gemm_q8_plan_info(int32_t m_rows, int64_t n_rows, int64_t k, int32_t *out4);
 int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t m_rows, int64_t k, const void *d_w_packed,
-                 const float *d_w_scale, int64_t n_rows, void *d_out, int32_t out_type, int64_t ldo, void *stream);
+                 const float *d_w_scale, int64_t n_rows, void *d_ws, size_t ws_bytes, void *d_out, int32_t out_type, int64_t ldo, void *stream);
 
 /* Measurement aid: while enabled, bita_verify_step brackets each of its GEMM launches with
  * a pair of HIP events on the caller's stream (not usable under graph capture).

@@ -19,7 +19,8 @@ EXPORTS = [
     "bita_gemm_workspace_bytes", "bita_gemm", "bita_gemm_noalloc_max_scratch_bytes", "bita_gemm_noalloc_scratch_bytes",
     "bita_gemm_noalloc", "bita_select", "bita_tune_gemm", "bita_gemm_plan_info", "bita_gemm_plan_detail", "bita_profile_enable",
     "bita_profile_disable", "bita_profile_read", "bita_last_error",
-    "bita_quantize_rows", "bita_norm_q8", "bita_silu_mul_q8", "bita_packed_q8_bytes", "bita_pack_weight_q8", "bita_gemm_q8",
+    "bita_quantize_rows", "bita_norm_q8", "bita_silu_mul_q8", "bita_packed_q8_bytes", "bita_pack_weight_q8",
+    "bita_gemm_q8_workspace_bytes", "bita_gemm_q8_plan_info", "bita_gemm_q8",
 ]
 
 
@@ -111,7 +112,9 @@ def lib():
     L.bita_silu_mul_q8.restype, L.bita_silu_mul_q8.argtypes = C.c_int, [vp, i32, i32, i64, i64, i32, vp, i64, vp, vp]
     L.bita_packed_q8_bytes.restype, L.bita_packed_q8_bytes.argtypes = sz, [i64, i64]
     L.bita_pack_weight_q8.restype, L.bita_pack_weight_q8.argtypes = C.c_int, [vp, i64, i64, i64, vp, i64, i64, i64, vp]
-    L.bita_gemm_q8.restype, L.bita_gemm_q8.argtypes = C.c_int, [vp, i64, vp, i32, i64, vp, vp, i64, vp, i32, i64, vp]
+    L.bita_gemm_q8_workspace_bytes.restype, L.bita_gemm_q8_workspace_bytes.argtypes = sz, [i32, i64, i64]
+    L.bita_gemm_q8_plan_info.restype, L.bita_gemm_q8_plan_info.argtypes = C.c_int, [i32, i64, i64, vp]
+    L.bita_gemm_q8.restype, L.bita_gemm_q8.argtypes = C.c_int, [vp, i64, vp, i32, i64, vp, vp, i64, vp, sz, vp, i32, i64, vp]
     _lib = L
     return L
 
@@ -616,9 +619,17 @@ def pack_weight_q8(src, dst=None, tile0=0, tile_stride=1, total_rows=None):
     return dst
 
 
-def gemm_q8(a, a_scale, w_packed, w_scale, n_rows, out=None, out_dtype=torch.float32):
+def gemm_q8_plan_info(m_rows, n_rows, k):
+    """{rows, cols (of a workgroup), splits (of k), skinny} that gemm_q8 of these sizes launches."""
+    out = (C.c_int32 * 4)()
+    _check(lib().bita_gemm_q8_plan_info(int(m_rows), int(n_rows), int(k), out))
+    return dict(rows=out[0], cols=out[1], splits=out[2], skinny=bool(out[3]))
+
+
+def gemm_q8(a, a_scale, w_packed, w_scale, n_rows, out=None, out_dtype=torch.float32, workspace=None):
     """a: int8 cuda [M][K] with its rows' scales (quantize_rows, norm_q8, silu_mul_q8); w_packed: pack_weight_q8 of an int8 [n_rows][K],
-    w_scale its rows' scales in packed order.  Returns [M][n_rows] in float32 or bfloat16, written into out where it is given."""
+    w_scale its rows' scales in packed order.  Returns [M][n_rows] in float32 or bfloat16, written into out where it is given.
+    workspace: a uint8 cuda tensor of bita_gemm_q8_workspace_bytes (allocated here when it is None and one is needed)."""
     lda = _matrix("a", a, (torch.int8,))
     m, k = a.shape
     if m == 1:
@@ -632,6 +643,10 @@ def gemm_q8(a, a_scale, w_packed, w_scale, n_rows, out=None, out_dtype=torch.flo
     if out is None:
         out = torch.empty((m, n_rows), dtype=out_dtype, device=a.device)
     ldo = _matrix("out", out, tuple(_F32_BF16), m, n_rows)
-    _same_device(a, a_scale, w_packed, w_scale, out)
-    _check(lib().bita_gemm_q8(_ptr(a), lda, _ptr(a_scale), m, k, _ptr(w_packed), _ptr(w_scale), n_rows, _ptr(out), _F32_BF16[out.dtype], ldo, _stream()))
+    _same_device(a, a_scale, w_packed, w_scale, out, workspace)
+    need = lib().bita_gemm_q8_workspace_bytes(m, n_rows, k)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=a.device)
+    _check(lib().bita_gemm_q8(_ptr(a), lda, _ptr(a_scale), m, k, _ptr(w_packed), _ptr(w_scale), n_rows, _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                              _ptr(out), _F32_BF16[out.dtype], ldo, _stream()))
     return out

@@ -20,7 +20,7 @@ NORM = dict(x=P, x_type=F32, m=4, d=64, ldx=64, delta=P, delta_type=BF16, ld_del
             scale=P, stream=None)
 GATE = dict(x=P, x_type=BF16, m=4, f=64, ldx=128, tile=16, q=P, ldq=64, scale=P, stream=None)
 PACK = dict(src=P, n=32, k=64, ld=64, dst=P, total=64, tile0=0, stride=1, stream=None)
-GEMM = dict(a=P, lda=64, a_scale=P, m=4, k=64, w=P, w_scale=P, n=64, out=P, out_type=F32, ldo=64, stream=None)
+GEMM = dict(a=P, lda=64, a_scale=P, m=4, k=64, w=P, w_scale=P, n=64, ws=None, ws_bytes=0, out=P, out_type=F32, ldo=64, stream=None)
 
 
 @pytest.mark.parametrize("name,good,bad,code", [
@@ -41,6 +41,8 @@ GEMM = dict(a=P, lda=64, a_scale=P, m=4, k=64, w=P, w_scale=P, n=64, out=P, out_
     ("bita_gemm_q8", GEMM, dict(w_scale=None), -1), ("bita_gemm_q8", GEMM, dict(out=None), -1), ("bita_gemm_q8", GEMM, dict(m=0), -1),
     ("bita_gemm_q8", GEMM, dict(n=0), -1), ("bita_gemm_q8", GEMM, dict(k=0), -1), ("bita_gemm_q8", GEMM, dict(out_type=3), -1),
     ("bita_gemm_q8", GEMM, dict(ldo=63), -1), ("bita_gemm_q8", GEMM, dict(lda=72), -1), ("bita_gemm_q8", GEMM, dict(lda=48), -1),
+    ("bita_gemm_q8", GEMM, dict(out=P + 2), -1), ("bita_gemm_q8", GEMM, dict(out=P + 1, out_type=BF16), -1), ("bita_gemm_q8", GEMM, dict(lda=(1 << 23) + 16), -4),
+    ("bita_gemm_q8", GEMM, dict(m=68, k=28672, lda=28672, n=8192, ldo=8192), -3), ("bita_gemm_q8", GEMM, dict(m=68, k=28672, lda=28672, n=8192, ldo=8192, ws=P, ws_bytes=1 << 16), -3),
     ("bita_gemm_q8", GEMM, dict(a=P + 8), -1), ("bita_gemm_q8", GEMM, dict(k=131072, lda=131088), -4),
 ])
 def test_refused_with_a_message(name, good, bad, code):
