@@ -2,6 +2,7 @@
 path runs in the HIP kernels of libbita.so.  torch supplies device memory and the
 current stream."""
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -511,33 +512,40 @@ def tree_attention(tmpl, q, k_cache, v_cache, k_tree, v_tree, prompt_k, prompt_v
 
 
 # ---- 8-bit linear layers ---------------------------------------------------------------------------------------------
+# (Called for every layer of a pass: arguments are looked at once each, pointers go over as integers.)
 _F32_BF16 = {torch.float32: 0, torch.bfloat16: 1}
+_I8 = {torch.int8: 2}
 
 
-def _matrix(name, t, types, rows=None, cols=None):
-    """t is a cuda matrix of one of these types and this size whose rows have neighbouring elements; its row stride."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in types):
-        raise ValueError(f"{name}: a cuda matrix of {' or '.join(str(x) for x in types)} is wanted")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols) or t.shape[0] < 1 or t.shape[1] < 1:
-        raise ValueError(f"{name}: {tuple(t.shape)}, wanted {rows if rows is not None else 'any'} x {cols if cols is not None else 'any'}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: the elements of a row have to be neighbours")
-    ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if ld < t.shape[1]:
-        raise ValueError(f"{name}: rows overlap (stride {ld})")
-    return ld
+# the current stream's handle (as in _stream)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _vector(name, t, n, dtype):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == 1 and t.shape[0] == n and t.is_contiguous()):
-        raise ValueError(f"{name}: a contiguous cuda vector of {n} {dtype} is wanted")
+@functools.lru_cache(4096)
+def _gemm_q8_scratch(m, n, k):
+    return lib().bita_gemm_q8_workspace_bytes(m, n, k)
 
 
-def _same_device(*ts):
-    dev = torch.cuda.current_device()
-    for t in ts:
-        if t is not None and t.device.index != dev:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+def _matrix(name, t, types, dev, rows=None, cols=None):
+    """Rows, columns and row stride of t, a matrix of one of these types (and this size) on the current device whose rows have
+    neighbouring elements and do not overlap."""
+    if t.dtype in types and t.dim() == 2 and t.get_device() == dev:
+        r, c = t.shape
+        ld, step = t.stride()
+        if r > 0 and c > 0 and (rows is None or r == rows) and (cols is None or c == cols) and (step == 1 or c == 1) and (ld >= c or r == 1):
+            return r, c, ld if r > 1 else c
+    raise ValueError(f"{name}: wanted {rows or 'any'} x {cols or 'any'} of {' or '.join(str(x) for x in types)} on cuda:{dev}, rows of neighbouring elements "
+                     f"that do not overlap; got {tuple(t.shape)} of {t.dtype} on {t.device}, strides {tuple(t.stride())}")
+
+
+def _vector(name, t, n, dtype, dev):
+    if not (t.dtype is dtype and t.get_device() == dev and t.dim() == 1 and t.numel() == n and (n < 2 or t.stride(0) == 1)):
+        raise ValueError(f"{name}: wanted {n} neighbouring {dtype} on cuda:{dev}; got {tuple(t.shape)} of {t.dtype} on {t.device}, strides {tuple(t.stride())}")
+
+
+def _bytes(name, t, n, dev):
+    if not (t.dtype is torch.uint8 and t.get_device() == dev and t.is_contiguous() and t.numel() >= n):
+        raise ValueError(f"{name}: wanted a contiguous buffer of {n} uint8 on cuda:{dev}; got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
 def empty_q8(rows, cols, device="cuda"):
@@ -545,57 +553,62 @@ def empty_q8(rows, cols, device="cuda"):
     return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
 
 
-def _q8_out(x, rows, cols, q, scale):
+def _q8_out(x, rows, cols, q, scale, dev):
     if q is None:
         q = empty_q8(rows, cols, x.device)
     if scale is None:
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-    ldq = _matrix("q", q, (torch.int8,), rows, cols)
-    _vector("scale", scale, rows, torch.float32)
-    return q, scale, ldq
+    else:
+        _vector("scale", scale, rows, torch.float32, dev)
+    return q, scale, _matrix("q", q, _I8, dev, rows, cols)[2]
 
 
 def quantize_rows(x, q=None, scale=None):
     """x: cuda [M][K], float32 or bfloat16.  Every row as 8-bit integers and a scale: (q int8 [M][K], scale fp32 [M]), written into
     q and scale where they are given."""
-    ldx = _matrix("x", x, tuple(_F32_BF16))
-    m, k = x.shape
-    q, scale, ldq = _q8_out(x, m, k, q, scale)
-    _same_device(x, q, scale)
-    _check(lib().bita_quantize_rows(_ptr(x), _F32_BF16[x.dtype], m, k, ldx, _ptr(q), ldq, _ptr(scale), _stream()))
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    m, k, ldx = _matrix("x", x, _F32_BF16, dev)
+    q, scale, ldq = _q8_out(x, m, k, q, scale, dev)
+    rc = L.bita_quantize_rows(x.data_ptr(), _F32_BF16[x.dtype], m, k, ldx, q.data_ptr(), ldq, scale.data_ptr(), _raw_stream(dev))
+    if rc:
+        _check(rc)
     return q, scale
 
 
 def norm_q8(x, gain, eps, delta=None, total=None, q=None, scale=None):
     """RMSNorm of x + delta times gain (bfloat16 [D]), rows as 8-bit integers: (q, scale).  x, delta: cuda [M][D], float32 or
     bfloat16.  With delta, x + delta is stored in total (x's type and size); total None: in x itself."""
-    ldx = _matrix("x", x, tuple(_F32_BF16))
-    m, d = x.shape
-    _vector("gain", gain, d, torch.bfloat16)
-    ldd = ldt = 0
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    m, d, ldx = _matrix("x", x, _F32_BF16, dev)
+    _vector("gain", gain, d, torch.bfloat16, dev)
+    pd = td = ldd = pt = ldt = 0
     if delta is not None:
-        ldd = _matrix("delta", delta, tuple(_F32_BF16), m, d)
+        ldd = _matrix("delta", delta, _F32_BF16, dev, m, d)[2]
+        pd, td = delta.data_ptr(), _F32_BF16[delta.dtype]
         total = x if total is None else total
-        ldt = _matrix("total", total, (x.dtype,), m, d)
+        ldt = _matrix("total", total, {x.dtype: 0}, dev, m, d)[2]
+        pt = total.data_ptr()
     elif total is not None:
         raise ValueError("total: there is nothing to store without delta")
-    q, scale, ldq = _q8_out(x, m, d, q, scale)
-    _same_device(x, gain, delta, total, q, scale)
-    _check(lib().bita_norm_q8(_ptr(x), _F32_BF16[x.dtype], m, d, ldx, _ptr(delta), 0 if delta is None else _F32_BF16[delta.dtype], ldd, _ptr(gain),
-                              float(eps), _ptr(total), ldt, _ptr(q), ldq, _ptr(scale), _stream()))
+    q, scale, ldq = _q8_out(x, m, d, q, scale, dev)
+    rc = L.bita_norm_q8(x.data_ptr(), _F32_BF16[x.dtype], m, d, ldx, pd, td, ldd, gain.data_ptr(), eps, pt, ldt, q.data_ptr(), ldq, scale.data_ptr(),
+                        _raw_stream(dev))
+    if rc:
+        _check(rc)
     return q, scale
 
 
 def silu_mul_q8(gate_up, tile=0, q=None, scale=None):
     """silu(gate) * up of gate_up, cuda [M][2F], float32 or bfloat16, rows as 8-bit integers: (q int8 [M][F], scale).  tile 16: tiles of
     16 gate columns, each followed by its 16 up columns, as a product with an interleaved weight leaves them; tile 0: all gate columns first."""
-    ldx = _matrix("gate_up", gate_up, tuple(_F32_BF16))
-    m, f = gate_up.shape[0], gate_up.shape[1] // 2
-    if gate_up.shape[1] % 2 or not f:
-        raise ValueError(f"gate_up: {gate_up.shape[1]} columns are not two halves")
-    q, scale, ldq = _q8_out(gate_up, m, f, q, scale)
-    _same_device(gate_up, q, scale)
-    _check(lib().bita_silu_mul_q8(_ptr(gate_up), _F32_BF16[gate_up.dtype], m, f, ldx, int(tile), _ptr(q), ldq, _ptr(scale), _stream()))
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    m, f2, ldx = _matrix("gate_up", gate_up, _F32_BF16, dev)
+    if f2 % 2:
+        raise ValueError(f"gate_up: {f2} columns are not two halves")
+    q, scale, ldq = _q8_out(gate_up, m, f2 // 2, q, scale, dev)
+    rc = L.bita_silu_mul_q8(gate_up.data_ptr(), _F32_BF16[gate_up.dtype], m, f2 // 2, ldx, tile, q.data_ptr(), ldq, scale.data_ptr(), _raw_stream(dev))
+    if rc:
+        _check(rc)
     return q, scale
 
 
@@ -606,16 +619,14 @@ def packed_q8_bytes(n_rows, k):
 def pack_weight_q8(src, dst=None, tile0=0, tile_stride=1, total_rows=None):
     """src: int8 cuda [N][K] (quantize_rows of a weight).  Returns the packed uint8 buffer (allocated here when dst is None,
     sized for total_rows rows)."""
-    ld = _matrix("src", src, (torch.int8,))
-    n, k = src.shape
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    n, k, ld = _matrix("src", src, _I8, dev)
     total_rows = total_rows or n
     need = packed_q8_bytes(total_rows, k)
     if dst is None:
         dst = torch.empty(need, dtype=torch.uint8, device=src.device)
-    elif not (dst.is_cuda and dst.dtype == torch.uint8 and dst.is_contiguous() and dst.numel() >= need):
-        raise ValueError(f"dst: a contiguous cuda buffer of {need} uint8 is wanted")
-    _same_device(src, dst)
-    _check(lib().bita_pack_weight_q8(_ptr(src), n, k, ld, _ptr(dst), total_rows, tile0, tile_stride, _stream()))
+    _bytes("dst", dst, need, dev)
+    _check(L.bita_pack_weight_q8(src.data_ptr(), n, k, ld, dst.data_ptr(), total_rows, tile0, tile_stride, _raw_stream(dev)))
     return dst
 
 
@@ -630,23 +641,31 @@ def gemm_q8(a, a_scale, w_packed, w_scale, n_rows, out=None, out_dtype=torch.flo
     """a: int8 cuda [M][K] with its rows' scales (quantize_rows, norm_q8, silu_mul_q8); w_packed: pack_weight_q8 of an int8 [n_rows][K],
     w_scale its rows' scales in packed order.  Returns [M][n_rows] in float32 or bfloat16, written into out where it is given.
     workspace: a uint8 cuda tensor of bita_gemm_q8_workspace_bytes (allocated here when it is None and one is needed)."""
-    lda = _matrix("a", a, (torch.int8,))
-    m, k = a.shape
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    m, k, lda = _matrix("a", a, _I8, dev)
+    k16, pa = (k + 15) & ~15, a.data_ptr()
     if m == 1:
-        lda = (lda + 15) // 16 * 16
-    if lda % 16 or a.data_ptr() % 16 or a.untyped_storage().nbytes() - a.storage_offset() < (m - 1) * lda + (k + 15) // 16 * 16:
+        lda = k16
+    if lda & 15 or pa & 15 or a.untyped_storage().nbytes() - a.storage_offset() < (m - 1) * lda + k16:
         raise ValueError("a: rows have to start at multiples of 16 bytes and to be readable to the next one behind their end (empty_q8)")
-    _vector("a_scale", a_scale, m, torch.float32)
-    _vector("w_scale", w_scale, n_rows, torch.float32)
-    if not (w_packed.is_cuda and w_packed.dtype == torch.uint8 and w_packed.is_contiguous() and w_packed.numel() >= packed_q8_bytes(n_rows, k)):
-        raise ValueError(f"w_packed: a contiguous cuda buffer of {packed_q8_bytes(n_rows, k)} uint8 is wanted")
+    _vector("a_scale", a_scale, m, torch.float32, dev)
+    _vector("w_scale", w_scale, n_rows, torch.float32, dev)
+    _bytes("w_packed", w_packed, (n_rows + 15 >> 4) * (k + 127 >> 7) * 2048, dev)
     if out is None:
         out = torch.empty((m, n_rows), dtype=out_dtype, device=a.device)
-    ldo = _matrix("out", out, tuple(_F32_BF16), m, n_rows)
-    _same_device(a, a_scale, w_packed, w_scale, out, workspace)
-    need = lib().bita_gemm_q8_workspace_bytes(m, n_rows, k)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=a.device)
-    _check(lib().bita_gemm_q8(_ptr(a), lda, _ptr(a_scale), m, k, _ptr(w_packed), _ptr(w_scale), n_rows, _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                              _ptr(out), _F32_BF16[out.dtype], ldo, _stream()))
+    ldo = _matrix("out", out, _F32_BF16, dev, m, n_rows)[2]
+    pw = nw = 0
+    if workspace is None:
+        nw = _gemm_q8_scratch(m, n_rows, k)
+        if nw:
+            workspace = torch.empty(nw, dtype=torch.uint8, device=a.device)
+    else:
+        _bytes("workspace", workspace, 0, dev)
+        nw = workspace.numel()
+    if nw:
+        pw = workspace.data_ptr()
+    rc = L.bita_gemm_q8(pa, lda, a_scale.data_ptr(), m, k, w_packed.data_ptr(), w_scale.data_ptr(), n_rows, pw, nw, out.data_ptr(), _F32_BF16[out.dtype],
+                        ldo, _raw_stream(dev))
+    if rc:
+        _check(rc)
     return out

@@ -1,5 +1,6 @@
 // The product of 8-bit integers with scales: Y[m][n] = (sum_k A[m][k] W[n][k]) sa[m] sw[n], sums in 32-bit integers.
 #include "common.h"
+#include <atomic>
 #include <cmath>
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -376,10 +377,21 @@ static PlanQ8 plan_q8(int m, int64_t n, int k_pairs) {
     return best;
 }
 
+// More LDS than the default limit has to be asked for, once for each kernel and device.
+struct LdsLimit { std::atomic<uint64_t> devices{0}; };
+static void raise_lds_limit(LdsLimit &done, const void *kernel, int bytes) {
+    int dev = 0;
+    if (bytes <= 65536 || hipGetDevice(&dev) != hipSuccess) return;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.devices.load(std::memory_order_relaxed) & bit)) return;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) done.devices.fetch_or(bit, std::memory_order_relaxed);
+}
+
 template <int MT, int WN, int KG, int P>
 static void launch_skinny(const GemmQ8 &g, const PlanQ8 &p) {
     constexpr int STAGES = 2 * MT * 8192, MERGE = KG > 1 ? KG * WN * MT * 1024 : 0, SMEM = STAGES > MERGE ? STAGES : MERGE;
-    (void)hipFuncSetAttribute((const void *)gemm_q8_skinny_kernel<MT, WN, KG, P>, hipFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    static LdsLimit limit;
+    raise_lds_limit(limit, (const void *)gemm_q8_skinny_kernel<MT, WN, KG, P>, SMEM);
     const int64_t tiles = (g.n + 15) / 16;
     hipLaunchKernelGGL((gemm_q8_skinny_kernel<MT, WN, KG, P>), dim3((unsigned)((tiles + WN - 1) / WN), (unsigned)((g.m + 16 * MT - 1) / (16 * MT)), p.splits),
                        dim3(WN * KG * 64), SMEM, g.s, g.a, g.lda, g.w, g.m, 2 * g.k_pairs, g.k16, g.n, g.sa, g.sw, g.out, g.ldo, g.out_type, p.split_steps,
@@ -392,7 +404,8 @@ template <int MF, int NF, int WM, int WN>
 static void launch_tile(const GemmQ8 &g) {
     constexpr int BM = 32 * MF * WM, BN = 32 * NF * WN, SMEM = 2 * (BM + BN) * 128;
     const int m_blocks = (int)(((int64_t)g.m + BM - 1) / BM), n_blocks = (int)((g.n + BN - 1) / BN), total = m_blocks * n_blocks;
-    (void)hipFuncSetAttribute((const void *)gemm_q8_tile_kernel<MF, NF, WM, WN>, hipFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    static LdsLimit limit;
+    raise_lds_limit(limit, (const void *)gemm_q8_tile_kernel<MF, NF, WM, WN>, SMEM);
     hipLaunchKernelGGL((gemm_q8_tile_kernel<MF, NF, WM, WN>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(WM * WN * 64), SMEM, g.s, g.a, g.lda, g.w, g.m,
                        g.k_pairs, g.k16, g.n, m_blocks, n_blocks, g.sa, g.sw, g.out, g.ldo, g.out_type);
 }
@@ -454,10 +467,11 @@ extern "C" int bita_pack_weight_q8(const int8_t *d_src, int64_t n_rows, int64_t 
     return BITA_OK;
 }
 
+static size_t plan_bytes(const PlanQ8 &p, int m, int64_t n) { return p.splits > 1 ? (size_t)p.splits * m * (size_t)((n + 15) / 16 * 16) * 4 : 0; }
+
 extern "C" size_t bita_gemm_q8_workspace_bytes(int32_t m_rows, int64_t n_rows, int64_t k) {
     if (m_rows <= 0 || n_rows <= 0 || k <= 0 || k > BITA_Q8_MAX_K) return 0;
-    const PlanQ8 p = plan_q8(m_rows, n_rows, (int)((k + 127) / 128));
-    return p.splits > 1 ? (size_t)p.splits * m_rows * (size_t)((n_rows + 15) / 16 * 16) * 4 : 0;
+    return plan_bytes(plan_q8(m_rows, n_rows, (int)((k + 127) / 128)), m_rows, n_rows);
 }
 
 extern "C" int bita_gemm_q8_plan_info(int32_t m_rows, int64_t n_rows, int64_t k, int32_t *out4) {
@@ -483,7 +497,7 @@ extern "C" int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_sca
         return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_gemm_q8: k %lld, lda %lld, at most %d and %d", (long long)k, (long long)lda, BITA_Q8_MAX_K, BITA_Q8_MAX_LD);
     const int k_pairs = (int)((k + 127) / 128), k16 = (int)((k + 15) / 16 * 16);
     const PlanQ8 p = plan_q8(m_rows, n_rows, k_pairs);
-    const size_t need = bita_gemm_q8_workspace_bytes(m_rows, n_rows, k);
+    const size_t need = plan_bytes(p, m_rows, n_rows);
     if (need && (!d_ws || ws_bytes < need || (uintptr_t)d_ws % 16))
         return bita_set_error(BITA_ERR_CAPACITY, "bita_gemm_q8: workspace %zu < %zu bytes, or not a multiple of 16", d_ws ? ws_bytes : (size_t)0, need);
     launch_gemm_q8(GemmQ8{d_a, lda, d_a_scale, m_rows, k_pairs, k16, (const i32x4 *)d_w_packed, d_w_scale, n_rows, d_out, out_type, ldo, (int *)d_ws, (hipStream_t)stream}, p);

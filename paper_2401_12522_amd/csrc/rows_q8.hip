@@ -9,19 +9,26 @@
 // and drops out of q, so that v stands for h_i g_i, which a double holds exactly (24 + 8 bits); whether |v| is above, on or below
 // the border (k + 1/2) a / 127 is whether 254 |v| - (2k + 1) a is positive, zero or negative, both terms exact in a double.
 //
-// One workgroup per row, which it holds in registers: one pass over memory, one barrier for the row's maximum and sum (the
-// gating's maximum is refined in double behind a second one).
+// One workgroup per row, whose values v it holds in registers as fp32: one pass over memory, one barrier for the row's maximum and sum
+// (the norm's and the gating's maximum is refined in double behind a second one: by the few threads that hold a candidate).  What bounds it is memory where there are many rows, provided
+// that a value costs few instructions and a row few waits: values in groups of eight a thread, one branch a group for all that is
+// rare, the waves' maxima and sums read side by side (one after the other they cost more than the row: 11008 rows of 4096 bf16
+// 91 us).
 #include "common.h"
 
 enum { ROWS_PLAIN = 0, ROWS_NORM = 1, ROWS_GATE = 2 };
 
-// |fp32 quotient - border| below which a code is found again in double: 127 times the relative error of the fp32 quotient,
-// which is at most 5 units of 2^-24 for the norm and plain rows, 8 for the gating (expf 1 ulp, sum, division, two products, the
-// factor 127 / a and its product) = 6e-5
+// fp32 quotients 127 |v| / a are found again in double where they are this near to a border: 127 times their relative error, at
+// most 5 units of 2^-24 for the norm and plain rows and 9 for the gating (exponential 2, sum 1/2, reciprocal 1, four roundings of
+// products and of 127 / a, and that division's) = 7e-5.
 #define ROUND_MARGIN 1.0e-4f
 // largest |v| of a row for which fp32 quotients have that error: 127 / a and all that matters are normal numbers
 #define PLAIN_RANGE_LO 1e-30f
 #define PLAIN_RANGE_HI 1e30f
+// gates below this are taken in double: exp(-gate) nears the end of fp32
+#define GATE_LOW -80.0f
+// rows from which on four waves take a row
+#define ROWS_MANY 1024
 
 struct RowsArgs {
     const void *x, *delta;            // ROWS_GATE: x holds gate and up columns
@@ -30,32 +37,34 @@ struct RowsArgs {
     int8_t *q;
     float *scale;
     int64_t ldx, ld_delta, ld_total, ldq;
-    int k, tile;                      // ROWS_GATE: columns of a gate tile (its up tile follows), k = one tile
+    int k, tile;                      // ROWS_GATE: columns of a gate tile (its up tile follows), 16 or k
     double eps;
 };
 
-__device__ __forceinline__ uint16_t to_bf16(float f) { return f != f ? (uint16_t)0x7FC0 : f32_to_bf16(f); }
+__device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }       // nearest even; a NaN stays one
 
-// 8 values of a row from column `at`; VEC: 16-byte loads (at and the row are multiples of 8 elements), else n of them singly
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void load8(const void *row, int64_t at, int n, float v[8]) {
-    if constexpr (VEC) {
-        if (n == 8) {
-            if constexpr (BF16) {
-                const uint4 u = *reinterpret_cast<const uint4 *>((const uint16_t *)row + at);
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// (16 and 8 bytes at an element's alignment: the hardware takes them)
+struct __attribute__((packed, aligned(2))) Halves8 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(4))) Words8 { float v[8]; };
+struct __attribute__((packed, aligned(1))) Bytes8 { uint32_t w[2]; };
+
+// n values of a row from column `at`, 8 but for the row's last
+template <bool BF16>
+__device__ __forceinline__ void load8(const void *row, int at, int n, float v[8]) {
+    if (n == 8) {
+        if constexpr (BF16) {
+            const Halves8 u = *reinterpret_cast<const Halves8 *>((const uint16_t *)row + at);
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    v[2 * e] = __uint_as_float(w[e] << 16);
-                    v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-                }
-            } else {
-                const float4 a = *reinterpret_cast<const float4 *>((const float *)row + at);
-                const float4 b = *reinterpret_cast<const float4 *>((const float *)row + at + 4);
-                v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            for (int e = 0; e < 4; e++) {
+                v[2 * e] = __uint_as_float(u.w[e] << 16);
+                v[2 * e + 1] = __uint_as_float(u.w[e] & 0xFFFF0000u);
             }
-            return;
+        } else {
+            const Words8 u = *reinterpret_cast<const Words8 *>((const float *)row + at);
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = u.v[e];
         }
+        return;
     }
 #pragma unroll
     for (int e = 0; e < 8; e++) {
@@ -63,21 +72,21 @@ __device__ __forceinline__ void load8(const void *row, int64_t at, int n, float 
         else v[e] = e < n ? ((const float *)row)[at + e] : 0.f;
     }
 }
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void store8(void *row, int64_t at, int n, const float v[8]) {
-    if constexpr (VEC) {
-        if (n == 8) {
-            if constexpr (BF16) {
-                uint32_t w[4];
+template <bool BF16>
+__device__ __forceinline__ void store8(void *row, int at, int n, const float v[8]) {
+    if (n == 8) {
+        if constexpr (BF16) {
+            Halves8 u;
 #pragma unroll
-                for (int e = 0; e < 4; e++) w[e] = (uint32_t)to_bf16(v[2 * e]) | ((uint32_t)to_bf16(v[2 * e + 1]) << 16);
-                *reinterpret_cast<uint4 *>((uint16_t *)row + at) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-                *reinterpret_cast<float4 *>((float *)row + at) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4 *>((float *)row + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
-            }
-            return;
+            for (int e = 0; e < 4; e++) u.w[e] = (uint32_t)to_bf16(v[2 * e]) | ((uint32_t)to_bf16(v[2 * e + 1]) << 16);
+            *reinterpret_cast<Halves8 *>((uint16_t *)row + at) = u;
+        } else {
+            Words8 u;
+#pragma unroll
+            for (int e = 0; e < 8; e++) u.v[e] = v[e];
+            *reinterpret_cast<Words8 *>((float *)row + at) = u;
         }
+        return;
     }
 #pragma unroll
     for (int e = 0; e < 8; e++)
@@ -87,13 +96,17 @@ __device__ __forceinline__ void store8(void *row, int64_t at, int n, const float
         }
 }
 
-__device__ __forceinline__ float gated(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+// silu(g) u = g u / (1 + exp(-g)) for g >= GATE_LOW: -g log2(e) in two words, so that the power of two is off by its own unit only
+__device__ __forceinline__ float gated(float g, float u) {
+    const float h = -g * 1.44269504f, l = __builtin_fmaf(-g, 1.92596303e-8f, __builtin_fmaf(-g, 1.44269504f, -h));
+    const float p = __builtin_amdgcn_exp2f(h), e = __builtin_fmaf(p, l * 0.693147181f, p);
+    return g * __builtin_amdgcn_rcpf(1.0f + e) * u;
+}
 __device__ __forceinline__ double gated_exactly(float g, float u) { return (double)g / (1.0 + exp(-(double)g)) * (double)u; }
 
-template <typename T>
-__device__ __forceinline__ T wave_max(T v) {
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+    for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
     return v;
 }
 __device__ __forceinline__ double wave_sum(double v) {
@@ -102,233 +115,269 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
+// fp32 + ROUNDER rounds to the nearest integer, ties to even, and has it (two's complement) in its low byte
+#define ROUNDER 12582912.0f
+
 // NV groups of 8 values per thread are held in registers.  KEEP false (rows longer than a workgroup holds; not the norm): the
-// groups go round and the row is read twice, the second time mostly from cache.
-template <int KIND, bool XB, bool DB, bool VEC, int NV, bool KEEP>
+// groups go round and the row is read again, mostly from cache.
+template <int KIND, bool XB, bool DB, int NV, bool KEEP>
 __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
     static_assert(KEEP || KIND != ROWS_NORM, "the norm holds its row");
-    __shared__ float s_max[16];
-    __shared__ double s_top[16], s_sum[16];
+    __shared__ uint32_t s_max[16];
+    __shared__ double s_sum[16];
     __shared__ unsigned long long s_exact;
-    const int row = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, waves = blockDim.x >> 6, k = a.k;
+    constexpr unsigned long long NO_NUMBER = ~0ull;
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, k = a.k;
     const char *x = (const char *)a.x + (int64_t)row * a.ldx * (XB ? 2 : 4);
     int8_t *q = a.q + (int64_t)row * a.ldq;
-    float h[NV][8], g[KIND == ROWS_NORM ? NV : 1][8];       // the row's values (ROWS_NORM: before the gain), and the gains
+    float h[NV][8];                                         // the row's values; ROWS_NORM: h g
 
     // (ROWS_GATE) the gate column of value `at`; its up column is a.tile further
     auto gate_column = [&](int at) __attribute__((always_inline)) { return a.tile == 16 ? ((at >> 4) << 5) + (at & 15) : at; };
-    auto one = [&](int col) __attribute__((always_inline)) {
-        return XB ? bf16_to_f32(((const uint16_t *)x)[col]) : ((const float *)x)[col];
-    };
+    auto one = [&](const void *p, int at) __attribute__((always_inline)) { return XB ? bf16_to_f32(((const uint16_t *)p)[at]) : ((const float *)p)[at]; };
+    // value `at` in double, from memory (ROWS_NORM: from what this thread stored there)
     auto exactly = [&](int at) __attribute__((always_inline)) {
-        const int col = gate_column(at);
-        return gated_exactly(one(col), one(col + a.tile));
+        if constexpr (KIND == ROWS_GATE) {
+            const int col = gate_column(at);
+            return gated_exactly(one(x, col), one(x, col + a.tile));
+        } else if constexpr (KIND == ROWS_PLAIN) {
+            return (double)one(x, at);
+        } else {
+            const float v = one(a.delta ? (const char *)a.total + (int64_t)row * a.ld_total * (XB ? 2 : 4) : x, at), g = bf16_to_f32(a.gain[at]);
+            const uint32_t bits = max(__float_as_uint(v) & 0x7FFFFFFFu, __float_as_uint(g) & 0x7FFFFFFFu);
+            return bits >= 0x7F800000u ? __longlong_as_double((long long)NO_NUMBER) : (double)v * (double)g;
+        }
     };
-
+    auto column = [&](int turn, int v) __attribute__((always_inline)) { return ((turn * NV + v) * (int)blockDim.x + tid) * 8; };
     auto fetch = [&](int v, int at) __attribute__((always_inline)) {
         const int n = min(max(k - at, 0), 8);
-        if (KIND == ROWS_GATE && n > 0) {
-            float u[8];
-            const int col = gate_column(at);
-            load8<XB, VEC>(x, col, n, h[v]);
-            load8<XB, VEC>(x, col + a.tile, n, u);
-#pragma unroll
-            for (int e = 0; e < 8; e++) h[v][e] = gated(h[v][e], u[e]);
-        } else if (n > 0) {
-            load8<XB, VEC>(x, at, n, h[v]);
-        } else {
+        if (n <= 0) {
 #pragma unroll
             for (int e = 0; e < 8; e++) h[v][e] = 0.f;
-        }
-        return n;
-    };
-
-    float top32 = 0.f;
-    double top = 0.0, sum = 0.0;
-    bool bad = false;
-    const int per_turn = NV * blockDim.x * 8, turns = KEEP ? 1 : (k + per_turn - 1) / per_turn;
-    for (int turn = 0; turn < turns; turn++) {
-#pragma unroll
-        for (int v = 0; v < NV; v++) {
-            const int at = turn * per_turn + (v * blockDim.x + tid) * 8;
-            const int n = fetch(v, at);
-            if constexpr (KIND == ROWS_NORM) {
-                if (n > 0) {
-                    load8<true, VEC>(a.gain, at, n, g[v]);
-                    if (a.delta) {
-                        float d[8];
-                        load8<DB, VEC>((const char *)a.delta + (int64_t)row * a.ld_delta * (DB ? 2 : 4), at, n, d);
-#pragma unroll
-                        for (int e = 0; e < 8; e++) {
-                            h[v][e] += d[e];
-                            if constexpr (XB) h[v][e] = bf16_to_f32(to_bf16(h[v][e]));     // (what is stored is what is normalised)
-                        }
-                        store8<XB, VEC>((char *)a.total + (int64_t)row * a.ld_total * (XB ? 2 : 4), at, n, h[v]);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; e++) g[v][e] = 0.f;
-                }
-            }
+        } else if constexpr (KIND == ROWS_GATE) {
+            float g[8], u[8];
+            const int col = gate_column(at);
+            load8<XB>(x, col, n, g);
+            load8<XB>(x, col + a.tile, n, u);
+            float least = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                if constexpr (KIND == ROWS_NORM) {
-                    const double hd = h[v][e], p = fabs(hd * (double)g[v][e]);
-                    bad |= !(p <= 1.7976931348623157e308);
-                    top = fmax(top, p);
+                h[v][e] = gated(g[e], u[e]);
+                least = fminf(least, g[e]);
+            }
+            if (least < GATE_LOW) {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (g[e] < GATE_LOW) h[v][e] = (float)gated_exactly(g[e], u[e]);
+            }
+        } else {
+            load8<XB>(x, at, n, h[v]);
+        }
+    };
+
+    // |v| as bits: any infinity or NaN is above every number
+    uint32_t top_bits = 0;
+    double sum = 0.0;
+    const int turns = KEEP ? 1 : (k + NV * (int)blockDim.x * 8 - 1) / (NV * (int)blockDim.x * 8);
+    for (int turn = 0; turn < turns; turn++) {
+#pragma unroll
+        for (int v = 0; v < NV; v++) fetch(v, column(turn, v));
+        if constexpr (KIND == ROWS_NORM) {
+            float d[NV][8];                                  // (all of a thread's reads are asked for before any is used)
+            if (a.delta) {
+#pragma unroll
+                for (int v = 0; v < NV; v++) {
+                    const int at = column(0, v), n = min(max(k - at, 0), 8);
+                    if (n > 0) load8<DB>((const char *)a.delta + (int64_t)row * a.ld_delta * (DB ? 2 : 4), at, n, d[v]);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                const int at = column(0, v), n = min(max(k - at, 0), 8);
+                if (n <= 0) continue;
+                float g[8];
+                load8<true>(a.gain, at, n, g);
+                if (a.delta) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        h[v][e] += d[v][e];
+                        if constexpr (XB) h[v][e] = bf16_to_f32(to_bf16(h[v][e]));         // (what is stored is what is normalised)
+                    }
+                    store8<XB>((char *)a.total + (int64_t)row * a.ld_total * (XB ? 2 : 4), at, n, h[v]);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const double hd = h[v][e];
                     sum = fma(hd, hd, sum);
-                } else {
-                    const float p = fabsf(h[v][e]);
-                    bad |= !(p <= 3.4028235e38f);
-                    top32 = fmaxf(top32, p);
+                    h[v][e] *= g[e];
                 }
             }
         }
+#pragma unroll
+        for (int v = 0; v < NV; v++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) top_bits = max(top_bits, __float_as_uint(h[v][e]) & 0x7FFFFFFFu);
     }
-    // the row's maximum (and sum of squares); a bad row's is NaN
-    if constexpr (KIND == ROWS_NORM) {
-        top = wave_max(top);
-        sum = wave_sum(sum);
-    } else {
-        top32 = wave_max(top32);
+    // the row's maximum (and sum of squares)
+    const uint32_t mine_bits = top_bits;
+    top_bits = wave_max(top_bits);
+    if constexpr (KIND == ROWS_NORM) sum = wave_sum(sum);
+    if (lane == 0) {
+        s_max[wave] = top_bits;
+        if constexpr (KIND == ROWS_NORM) s_sum[wave] = sum;
     }
-    const bool wave_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
-    if ((tid & 63) == 0) {
-        s_max[wave] = wave_bad ? __builtin_nanf("") : top32;
-        s_top[wave] = top;
-        s_sum[wave] = sum;
-    }
-    if (tid == 0) s_exact = 0;
+    if (KIND != ROWS_PLAIN && tid == 0) s_exact = 0;
     __syncthreads();
-    top32 = 0.f;
-    top = sum = 0.0;
-    bad = false;
-    for (int w = 0; w < waves; w++) {
-        bad |= s_max[w] != s_max[w];
-        top32 = fmaxf(top32, s_max[w]);
-        top = fmax(top, s_top[w]);
-        sum += s_sum[w];
+    {
+        const bool some = (lane & 15) < waves;               // 16 lanes take a wave's result each
+        top_bits = some ? s_max[lane & 15] : 0;
+        if constexpr (KIND == ROWS_NORM) sum = some ? s_sum[lane & 15] : 0.0;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) {
+            top_bits = max(top_bits, (uint32_t)__shfl_xor((int)top_bits, o, 64));
+            if constexpr (KIND == ROWS_NORM) sum += __shfl_xor(sum, o, 64);
+        }
     }
-    if constexpr (KIND == ROWS_NORM) top32 = (float)top;
-    else top = top32;
+    bool bad = top_bits >= 0x7F800000u;
+    const float top32 = __uint_as_float(top_bits);
     const bool in_range = top32 >= PLAIN_RANGE_LO && top32 <= PLAIN_RANGE_HI;
-    if constexpr (KIND == ROWS_GATE) {
-        // the largest value in double: of those that fp32 has within its error of its largest
+    double top = top32;
+    if constexpr (KIND != ROWS_PLAIN) {
+        // the largest value in double: of those that fp32 has within its error of its largest (all, where fp32 does not hold them)
         const float near = in_range ? top32 * (1.0f - 1e-5f) : 0.f;
-        double best = 0.0;
-        for (int turn = 0; turn < turns; turn++)
+        if (!in_range || __uint_as_float(mine_bits) >= near) {
+            unsigned long long best = 0;
+            for (int turn = 0; turn < turns; turn++) {
+                uint64_t todo = 0;
 #pragma unroll
-            for (int v = 0; v < NV; v++) {
-                const int at = turn * per_turn + (v * blockDim.x + tid) * 8;
-                if constexpr (!KEEP) fetch(v, at);
+                for (int v = 0; v < NV; v++) {
+                    const int at = column(turn, v);
+                    if constexpr (!KEEP) fetch(v, at);
 #pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (at + e < k && fabsf(h[v][e]) >= near) best = fmax(best, fabs(exactly(at + e)));
+                    for (int e = 0; e < 8; e++)
+                        if (at + e < k && (!in_range || fabsf(h[v][e]) >= near)) todo |= 1ull << (8 * v + e);
+                }
+                while (todo) {
+                    const int i = __builtin_ctzll(todo);
+                    todo &= todo - 1;
+                    const unsigned long long w = (unsigned long long)__double_as_longlong(exactly(column(turn, i >> 3) + (i & 7)));
+                    best = max(best, w == NO_NUMBER ? w : w & ~(1ull << 63));
+                }
             }
-        if (best > 0.0) atomicMax(&s_exact, (unsigned long long)__double_as_longlong(best));
+            if (best) atomicMax(&s_exact, best);
+        }
         __syncthreads();
         top = __longlong_as_double((long long)s_exact);
+        if constexpr (KIND == ROWS_NORM) bad = s_exact == NO_NUMBER;
     }
     if (tid == 0) {
         double s = top / 127.0;
         if constexpr (KIND == ROWS_NORM) s /= sqrt(sum / (double)k + a.eps);
         a.scale[row] = bad ? __builtin_nanf("") : top == 0.0 ? 0.f : (float)s;
     }
-    const bool zero = bad || top == 0.0;
+    const bool none = bad || top == 0.0;
     const float c32 = 127.0f / top32;
-    auto code = [&](int v, int e, int at) __attribute__((always_inline)) {
-        float p32 = h[v][e];
-        if constexpr (KIND == ROWS_NORM) p32 *= g[v][e];
-        const float t = p32 * c32;
-        float r = rintf(t);
-        if (!in_range || fabsf(t - r) > 0.5f - ROUND_MARGIN) {
-            if constexpr (KIND == ROWS_GATE) {
-                r = at + e < k ? (float)rint(exactly(at + e) * 127.0 / top) : 0.f;
-            } else {
-                double p = h[v][e];
-                if constexpr (KIND == ROWS_NORM) p *= (double)g[v][e];
-                const double m = fabs(p), low = floor(m * (127.0 / top)), off = fma(-(2.0 * low + 1.0), top, 254.0 * m);
-                const double up = off > 0.0 || (off == 0.0 && ((int)low & 1)) ? low + 1.0 : low;
-                r = (float)copysign(up, p);
-            }
-        }
-        return zero ? 0 : (int)r;
-    };
-    for (int turn = 0; turn < turns; turn++)
+    for (int turn = 0; turn < turns; turn++) {
+        uint64_t todo = 0;                                   // values whose integer is found in double
 #pragma unroll
         for (int v = 0; v < NV; v++) {
-            const int at = turn * per_turn + (v * blockDim.x + tid) * 8;
+            const int at = column(turn, v);
             if constexpr (!KEEP) fetch(v, at);
             const int n = min(max(k - at, 0), 8);
             if (n <= 0) continue;
-            int c[8];
+            float r[8], off = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; e++) c[e] = code(v, e, at);
-            if (VEC && n == 8) {
-                uint2 w;
-                w.x = (c[0] & 255) | (c[1] & 255) << 8 | (c[2] & 255) << 16 | (uint32_t)c[3] << 24;
-                w.y = (c[4] & 255) | (c[5] & 255) << 8 | (c[6] & 255) << 16 | (uint32_t)c[7] << 24;
-                *reinterpret_cast<uint2 *>(q + at) = w;
+            for (int e = 0; e < 8; e++) {
+                const float t = h[v][e] * c32;
+                r[e] = t + ROUNDER;
+                off = fmaxf(off, fabsf(t - (r[e] - ROUNDER)));
+            }
+            if (!in_range) todo |= (uint64_t)((1 << n) - 1) << (8 * v);
+            else if (off > 0.5f - ROUND_MARGIN) {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (e < n && fabsf(h[v][e] * c32 - (r[e] - ROUNDER)) > 0.5f - ROUND_MARGIN) todo |= 1ull << (8 * v + e);
+            }
+            uint32_t b[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) b[e] = __float_as_uint(r[e]);
+            if (n == 8) {
+                Bytes8 w;
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const uint32_t lo = __builtin_amdgcn_perm(b[4 * e + 1], b[4 * e], 0x0c0c0400), hi = __builtin_amdgcn_perm(b[4 * e + 3], b[4 * e + 2], 0x0c0c0400);
+                    w.w[e] = none ? 0u : lo | hi << 16;
+                }
+                *reinterpret_cast<Bytes8 *>(q + at) = w;
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e++)
-                    if (e < n) q[at + e] = (int8_t)c[e];
+                    if (e < n) q[at + e] = none ? 0 : (int8_t)(b[e] & 255);
             }
         }
+        while (todo && !none) {
+            const int i = __builtin_ctzll(todo), at = column(turn, i >> 3) + (i & 7);
+            todo &= todo - 1;
+            const double p = exactly(at), m = fabs(p);
+            double up;
+            if constexpr (KIND == ROWS_GATE) {
+                up = rint(m * 127.0 / top);
+            } else {
+                const double low = floor(m * (127.0 / top)), over = fma(-(2.0 * low + 1.0), top, 254.0 * m);
+                up = over > 0.0 || (over == 0.0 && ((int)low & 1)) ? low + 1.0 : low;
+            }
+            q[at] = (int8_t)(int)copysign(up, p);
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------
-#define ROWS_HELD 4                    // groups of 8 values a thread holds at most
-template <int KIND, bool XB, bool DB, bool VEC>
-static void launch_rows_nv(const RowsArgs &a, int m, hipStream_t s) {
-    const int groups = (a.k + 7) / 8, held = (groups + 1023) / 1024;
-    const int nv = held <= 1 ? 1 : held <= 2 ? 2 : 4;
-    const int threads = min(1024, ((groups + nv - 1) / nv + 63) / 64 * 64);
-    if (nv == 1) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, VEC, 1, true>), dim3(m), dim3(threads), 0, s, a);
-    else if (nv == 2) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, VEC, 2, true>), dim3(m), dim3(threads), 0, s, a);
-    else if constexpr (KIND != ROWS_NORM) {
-        if (held <= ROWS_HELD) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, VEC, 4, true>), dim3(m), dim3(threads), 0, s, a);
-        else hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, VEC, 2, false>), dim3(m), dim3(1024), 0, s, a);
-    }
-}
 template <int KIND, bool XB, bool DB>
-static void launch_rows(const RowsArgs &a, int m, bool vec, hipStream_t s) {
-    if (vec) launch_rows_nv<KIND, XB, DB, true>(a, m, s);
-    else launch_rows_nv<KIND, XB, DB, false>(a, m, s);
+static void launch_rows(const RowsArgs &a, int m, hipStream_t s) {
+    // Few rows: as many waves as there are groups, for a row is latency.  Many: four waves and several rows a CU, up to four groups a
+    // thread for plain rows and two for the others, which compute more (four / two: 28672 rows of 8192 134 / 150 us; norm of 8192 rows of
+    // 8192 fp32 195 / 178, 4096 gated rows of 28672 172 / 165; one: 11008 rows of 4096 30 -> 36, norm of 8192 rows of 5120 78 -> 96).
+    constexpr int HELD = KIND == ROWS_PLAIN ? 4 : 2;
+    const int groups = (a.k + 7) / 8, most = m >= ROWS_MANY ? 256 : 1024, needed = (groups + HELD - 1) / HELD;
+    const int threads = max(min(most, (groups + 63) / 64 * 64), min(1024, (needed + 63) / 64 * 64)), nv = (groups + threads - 1) / threads;
+#define ROWS_LAUNCH(NV, KEEP) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, NV, KEEP>), dim3(m), dim3(threads), 0, s, a)
+    if (nv <= 1) ROWS_LAUNCH(1, true);
+    else if (KIND == ROWS_NORM || nv <= 2) ROWS_LAUNCH(2, true);      // (1024 threads of two groups: the norm's longest row)
+    else if constexpr (KIND != ROWS_NORM) {
+        if (nv <= 4) ROWS_LAUNCH(4, true);
+        else ROWS_LAUNCH(2, false);
+    }
+#undef ROWS_LAUNCH
 }
 
-// (a single row has no stride)
-static bool aligned(const void *p, int64_t ld, int64_t size, int m, int to) { return (uintptr_t)p % to == 0 && (m == 1 || ld * size % to == 0); }
 static bool type_ok(int32_t t) { return t == BITA_F32 || t == BITA_BF16; }
-static int64_t type_size(int32_t t) { return t == BITA_BF16 ? 2 : 4; }
+static bool at_element(const void *p, int32_t t) { return (uintptr_t)p % (t == BITA_BF16 ? 2 : 4) == 0; }
 
 extern "C" int bita_quantize_rows(const void *d_x, int32_t x_type, int32_t m_rows, int64_t k, int64_t ldx, int8_t *d_q, int64_t ldq,
                                   float *d_scale, void *stream) {
-    if (!d_x || !d_q || !d_scale || m_rows <= 0 || k <= 0 || !type_ok(x_type) || ldx < k || ldq < k)
+    if (!d_x || !d_q || !d_scale || m_rows <= 0 || k <= 0 || !type_ok(x_type) || !at_element(d_x, x_type) || ldx < k || ldq < k)
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_quantize_rows: bad argument");
     if (k > BITA_Q8_MAX_K) return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_quantize_rows: k %lld, at most %d", (long long)k, BITA_Q8_MAX_K);
     RowsArgs a = {};
     a.x = d_x; a.q = d_q; a.scale = d_scale; a.ldx = ldx; a.ldq = ldq; a.k = (int)k;
-    const bool vec = aligned(d_x, ldx, type_size(x_type), m_rows, 16) && aligned(d_q, ldq, 1, m_rows, 8);
-    if (x_type == BITA_BF16) launch_rows<ROWS_PLAIN, true, false>(a, m_rows, vec, (hipStream_t)stream);
-    else launch_rows<ROWS_PLAIN, false, false>(a, m_rows, vec, (hipStream_t)stream);
+    if (x_type == BITA_BF16) launch_rows<ROWS_PLAIN, true, false>(a, m_rows, (hipStream_t)stream);
+    else launch_rows<ROWS_PLAIN, false, false>(a, m_rows, (hipStream_t)stream);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
 }
 
 extern "C" int bita_silu_mul_q8(const void *d_gate_up, int32_t x_type, int32_t m_rows, int64_t d_ffn, int64_t ldx, int32_t tile,
                                 int8_t *d_q, int64_t ldq, float *d_scale, void *stream) {
-    if (!d_gate_up || !d_q || !d_scale || m_rows <= 0 || d_ffn <= 0 || !type_ok(x_type) || ldx < 2 * d_ffn || ldq < d_ffn)
+    if (!d_gate_up || !d_q || !d_scale || m_rows <= 0 || d_ffn <= 0 || !type_ok(x_type) || !at_element(d_gate_up, x_type) ||
+        ldx < 2 * d_ffn || ldq < d_ffn)
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_silu_mul_q8: bad argument");
     if ((tile != 0 && tile != 16) || (tile == 16 && d_ffn % 16))
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_silu_mul_q8: tile must be 0 (all gate columns first) or 16 (d_ffn a multiple of 16)");
     if (d_ffn > BITA_Q8_MAX_K) return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_silu_mul_q8: d_ffn %lld, at most %d", (long long)d_ffn, BITA_Q8_MAX_K);
     RowsArgs a = {};
     a.x = d_gate_up; a.q = d_q; a.scale = d_scale; a.ldx = ldx; a.ldq = ldq; a.k = (int)d_ffn; a.tile = tile ? tile : (int)d_ffn;
-    const int64_t size = type_size(x_type);
-    const bool vec = aligned(d_gate_up, ldx, size, m_rows, 16) && a.tile * size % 16 == 0 && aligned(d_q, ldq, 1, m_rows, 8);
-    if (x_type == BITA_BF16) launch_rows<ROWS_GATE, true, false>(a, m_rows, vec, (hipStream_t)stream);
-    else launch_rows<ROWS_GATE, false, false>(a, m_rows, vec, (hipStream_t)stream);
+    if (x_type == BITA_BF16) launch_rows<ROWS_GATE, true, false>(a, m_rows, (hipStream_t)stream);
+    else launch_rows<ROWS_GATE, false, false>(a, m_rows, (hipStream_t)stream);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
 }
@@ -336,8 +385,9 @@ extern "C" int bita_silu_mul_q8(const void *d_gate_up, int32_t x_type, int32_t m
 extern "C" int bita_norm_q8(const void *d_x, int32_t x_type, int32_t m_rows, int64_t d, int64_t ldx, const void *d_delta,
                             int32_t delta_type, int64_t ld_delta, const void *d_gain, float eps, void *d_total, int64_t ld_total,
                             int8_t *d_q, int64_t ldq, float *d_scale, void *stream) {
-    if (!d_x || !d_gain || !d_q || !d_scale || m_rows <= 0 || d <= 0 || !type_ok(x_type) || ldx < d || ldq < d || !(eps >= 0.f) ||
-        (d_delta && (!type_ok(delta_type) || ld_delta < d || !d_total || ld_total < d)))
+    if (!d_x || !d_gain || !d_q || !d_scale || m_rows <= 0 || d <= 0 || !type_ok(x_type) || !at_element(d_x, x_type) ||
+        !at_element(d_gain, BITA_BF16) || ldx < d || ldq < d || !(eps >= 0.f) ||
+        (d_delta && (!type_ok(delta_type) || !at_element(d_delta, delta_type) || !at_element(d_total, x_type) || ld_delta < d || !d_total || ld_total < d)))
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_norm_q8: bad argument");
     if (d > 1024 * RMS_MAX_CHUNKS)
         return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_norm_q8: d %lld, at most %d", (long long)d, 1024 * RMS_MAX_CHUNKS);
@@ -346,17 +396,14 @@ extern "C" int bita_norm_q8(const void *d_x, int32_t x_type, int32_t m_rows, int
     RowsArgs a = {};
     a.x = d_x; a.delta = d_delta; a.gain = (const uint16_t *)d_gain; a.total = d_total; a.q = d_q; a.scale = d_scale;
     a.ldx = ldx; a.ld_delta = ld_delta; a.ld_total = ld_total; a.ldq = ldq; a.k = (int)d; a.eps = (double)eps;
-    const int64_t size = type_size(x_type);
-    const bool vec = aligned(d_x, ldx, size, m_rows, 16) && (uintptr_t)d_gain % 16 == 0 && aligned(d_q, ldq, 1, m_rows, 8) &&
-                     (!d_delta || (aligned(d_delta, ld_delta, type_size(delta_type), m_rows, 16) && aligned(d_total, ld_total, size, m_rows, 16)));
     hipStream_t s = (hipStream_t)stream;
     const bool db = d_delta && delta_type == BITA_BF16;
     if (x_type == BITA_BF16) {
-        if (db) launch_rows<ROWS_NORM, true, true>(a, m_rows, vec, s);
-        else launch_rows<ROWS_NORM, true, false>(a, m_rows, vec, s);
+        if (db) launch_rows<ROWS_NORM, true, true>(a, m_rows, s);
+        else launch_rows<ROWS_NORM, true, false>(a, m_rows, s);
     } else {
-        if (db) launch_rows<ROWS_NORM, false, true>(a, m_rows, vec, s);
-        else launch_rows<ROWS_NORM, false, false>(a, m_rows, vec, s);
+        if (db) launch_rows<ROWS_NORM, false, true>(a, m_rows, s);
+        else launch_rows<ROWS_NORM, false, false>(a, m_rows, s);
     }
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
