@@ -64,6 +64,8 @@ def parse_args():
     ap.add_argument("--mode", default="planted", choices=["free", "planted"])
     ap.add_argument("--page-size", type=int, default=0,
                     help="keep the KV cache in shuffled pages of this many slots (power of two >= 16; runs free)")
+    ap.add_argument("--int8", action="store_true",
+                    help="8-bit layers (weights and the rows in front of each product as 8-bit integers with scales; LM head bf16)")
     ap.add_argument("--no-graph", action="store_true")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--seed", type=int, default=0)
@@ -227,7 +229,7 @@ def run_workload(args, workload, steps, warmup, want_cpu_baseline):
                 wsrc_np[(n, l)] = w.numpy(n, l)
         for n in ("tok_emb", "mask_emb", "lm_head", "final_norm"):
             wsrc_np[(n, None)] = w.numpy(n)
-    model = bita.Model(cfg, w, max_pos=smax + 64, free_source=True)
+    model = bita.Model(cfg, w, max_pos=smax + 64, free_source=True, int8=args.int8)
     tmpl = bita.TreeTemplate(tin.parent, tin.is_mask, tin.n_tree, cfg.n_mask)
     if args.page_size:
         kv = bita.PagedKVState(cfg, cfg.n_layers, NB, smax, R, args.page_size, seed=args.seed)
@@ -387,7 +389,8 @@ def run_workload(args, workload, steps, warmup, want_cpu_baseline):
     grown = np.concatenate([np.zeros((1, NB), np.int64), np.cumsum(nacc[warmup:], axis=0)[:-1]])
     ctx_lens = ctx_start[None, :] + grown                      # [steps][batch] context length seen by each step
     kv_bytes = float(np.mean([cfg.kv_bytes([int(c) for c in row]) for row in ctx_lens]))
-    bytes_per_step = cfg.weight_bytes() + kv_bytes
+    layer_bytes = cfg.weight_bytes() - 2 * cfg.vocab * cfg.d_model
+    bytes_per_step = cfg.weight_bytes() - (layer_bytes // 2 if args.int8 else 0) + kv_bytes
     gbps = bytes_per_step / (ms_per_step * 1e-3) / 1e9
 
     # ---- spread of the step time: the same run once more, an event behind every step -----------
@@ -416,9 +419,10 @@ def run_workload(args, workload, steps, warmup, want_cpu_baseline):
     g_ms, g_bytes = B.profile_read(n_gemm * prof_steps)
     gemm_avg_us = float(np.mean(g_ms)) * 1e3
     gemm_gbps = float(np.sum(g_bytes)) / (float(np.sum(g_ms)) * 1e-3) / 1e9
-    standard = R == 68 and NB == 1 and not args.page_size
+    standard = R == 68 and NB == 1 and not args.page_size and not args.int8
     prof_file, prof_gemm_us = ROCPROF_GEMM.get(workload, (None, None))
-    roofline = {"bound": "hbm", "kernel": "gemm_skinny_kernel (all %d launches of a step)" % n_gemm,
+    roofline = {"bound": "hbm", "kernel": "%s (all %d launches of a step)" % ("8-bit products and the LM head's gemm_skinny_kernel" if args.int8
+                                                                             else "gemm_skinny_kernel", n_gemm),
                 "achieved": gemm_gbps, "peak": HBM_PEAK_GBPS, "unit": "GB/s", "frac": gemm_gbps / HBM_PEAK_GBPS,
                 "frac_source": "HIP events recorded by the library around every GEMM launch on the launch stream, "
                                "%d eager steps run right after the timed graph replays (an event pair adds about "
@@ -438,7 +442,7 @@ def run_workload(args, workload, steps, warmup, want_cpu_baseline):
     out = {
         "metric": "tree_verify_scored_tokens_per_s", "value": R * NB * steps / wall, "unit": "tokens/s",
         "n_gpus": 1, "steps": steps, "warmup": warmup, "ms_per_step": ms_per_step,
-        "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "bf16",
+        "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "int8" if args.int8 else "bf16",
         "data": "synthetic",
         "config": {"workload": f"llama2-{workload}-shaped random-init, ctx {ctx_n}, batch {NB}, "
                                f"{tin.n_tree}-node tree ({args.tree or 'default'}) + {R - tin.n_tree} mask rows, P={cfg.n_prompt}, mode {args.mode}",
@@ -469,8 +473,8 @@ def main():
               file=sys.stderr)
         sys.exit(2)
     headline = args.workload or "7b"
-    out = run_workload(args, headline, args.steps, args.warmup, not args.no_cpu_baseline)
-    plain = args.batch == 1 and not args.tree and not args.page_size and args.mode == "planted" and not args.ctx
+    out = run_workload(args, headline, args.steps, args.warmup, not args.no_cpu_baseline and not args.int8)
+    plain = args.batch == 1 and not args.tree and not args.page_size and args.mode == "planted" and not args.ctx and not args.int8
     if args.workload is None and not args.no_second_leg and plain:
         import gc
         import torch

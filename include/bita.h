@@ -370,6 +370,17 @@ int bita_gemm_q8_plan_info(int32_t m_rows, int64_t n_rows, int64_t k, int32_t *o
 int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t m_rows, int64_t k, const void *d_w_packed,
                  const float *d_w_scale, int64_t n_rows, void *d_ws, size_t ws_bytes, void *d_out, int32_t out_type, int64_t ldo, void *stream);
 
+/* A model whose layers' matrices are 8-bit: wqkv, wo, w_gate_up and w_down of `w` packed by bita_pack_weight_q8 in the arrangement
+ * of bita_weights, and the fp32 scales of their rows in the same order (gate/up: tiles of 16 in turn).  Everything else is as for
+ * bita_model_create: embeddings, norms, prompt prefix and LM head in bf16, the K/V cache too.  Every call that takes a
+ * model takes this one; each layer runs bita_norm_q8, bita_gemm_q8, attention, bita_quantize_rows (the attention output as bf16),
+ * bita_gemm_q8, bita_norm_q8, bita_gemm_q8, bita_silu_mul_q8 and bita_gemm_q8.  A row's integers are its own, so drafted and plain
+ * decoding see the same model.  n_heads * head_dim and d_ffn at most BITA_Q8_MAX_K.  The members are HOST arrays of n_layers device pointers. */
+typedef struct bita_scales_q8 {
+    const float *const *wqkv, *const *wo, *const *w_gate_up, *const *w_down;
+} bita_scales_q8;
+int bita_model_create_q8(const bita_config *cfg, const bita_weights *w, const bita_scales_q8 *scales, bita_model **out);
+
 /* Measurement aid: while enabled, bita_verify_step brackets each of its GEMM launches with
  * a pair of HIP events on the caller's stream (not usable under graph capture).
  * bita_profile_enable creates the events (up to max_records launches are recorded from the

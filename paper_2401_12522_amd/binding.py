@@ -21,7 +21,7 @@ EXPORTS = [
     "bita_gemm_noalloc", "bita_select", "bita_tune_gemm", "bita_gemm_plan_info", "bita_gemm_plan_detail", "bita_profile_enable",
     "bita_profile_disable", "bita_profile_read", "bita_last_error",
     "bita_quantize_rows", "bita_norm_q8", "bita_silu_mul_q8", "bita_packed_q8_bytes", "bita_pack_weight_q8",
-    "bita_gemm_q8_workspace_bytes", "bita_gemm_q8_plan_info", "bita_gemm_q8",
+    "bita_model_create_q8", "bita_gemm_q8_workspace_bytes", "bita_gemm_q8_plan_info", "bita_gemm_q8",
 ]
 
 
@@ -41,6 +41,10 @@ class _Weights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("tok_emb", "mask_emb", "final_norm", "lm_head")] + \
                [(n, C.POINTER(C.c_void_p)) for n in ("attn_norm", "ffn_norm", "wqkv", "wo", "w_gate_up",
                                                      "w_down", "prompt_k", "prompt_v")]
+
+
+class _ScalesQ8(C.Structure):
+    _fields_ = [(n, C.POINTER(C.c_void_p)) for n in ("wqkv", "wo", "w_gate_up", "w_down")]
 
 
 class _KV(C.Structure):
@@ -113,6 +117,8 @@ def lib():
     L.bita_silu_mul_q8.restype, L.bita_silu_mul_q8.argtypes = C.c_int, [vp, i32, i32, i64, i64, i32, vp, i64, vp, vp]
     L.bita_packed_q8_bytes.restype, L.bita_packed_q8_bytes.argtypes = sz, [i64, i64]
     L.bita_pack_weight_q8.restype, L.bita_pack_weight_q8.argtypes = C.c_int, [vp, i64, i64, i64, vp, i64, i64, i64, vp]
+    L.bita_model_create_q8.restype = C.c_int
+    L.bita_model_create_q8.argtypes = [C.POINTER(_Config), C.POINTER(_Weights), C.POINTER(_ScalesQ8), C.POINTER(vp)]
     L.bita_gemm_q8_workspace_bytes.restype, L.bita_gemm_q8_workspace_bytes.argtypes = sz, [i32, i64, i64]
     L.bita_gemm_q8_plan_info.restype, L.bita_gemm_q8_plan_info.argtypes = C.c_int, [i32, i64, i64, vp]
     L.bita_gemm_q8.restype, L.bita_gemm_q8.argtypes = C.c_int, [vp, i64, vp, i32, i64, vp, vp, i64, vp, sz, vp, i32, i64, vp]
@@ -173,10 +179,11 @@ class TreeTemplate:
 class Model:
     """Packs the matrices of a weight source (anything with .torch(name, layer) giving bf16
     cuda tensors [out][in]) and creates the library handle.  The packed buffers and the
-    small row-major tensors are kept alive here; the library only borrows them."""
+    small row-major tensors are kept alive here; the library only borrows them.
+    int8: the layers' matrices as 8-bit integers, one scale for each of their rows (the LM head stays bfloat16)."""
 
-    def __init__(self, cfg, weights, max_pos, n_layers=None, free_source=False):
-        self.cfg = cfg
+    def __init__(self, cfg, weights, max_pos, n_layers=None, free_source=False, int8=False):
+        self.cfg, self.int8 = cfg, bool(int8)
         L = cfg.n_layers if n_layers is None else n_layers
         self.n_layers = L
         dev = torch.device("cuda")
@@ -197,6 +204,19 @@ class Model:
             keep.append(dst)
             return dst
 
+        def pack_many_q8(parts, k, interleave=False):
+            total = sum(p.shape[0] for p in parts)
+            dst = torch.empty(packed_q8_bytes(total, k), dtype=torch.uint8, device=dev)
+            scales, row = [], 0
+            for i, p in enumerate(parts):
+                q, s = quantize_rows(p.contiguous())
+                pack_weight_q8(q, dst, i if interleave else row // 16, len(parts) if interleave else 1, total_rows=total)
+                scales.append(s.view(-1, 16) if interleave else s)
+                row += p.shape[0]
+            scale = torch.stack(scales, 1).reshape(-1) if interleave else torch.cat(scales)
+            keep.extend((dst, scale))
+            return dst, scale
+
         def small(name, layer=None):
             t = weights.torch(name, layer).to(dev).contiguous()
             keep.append(t)
@@ -207,12 +227,18 @@ class Model:
             keep.append(a)
             return a
         cols = {n: [] for n in ("attn_norm", "ffn_norm", "wqkv", "wo", "w_gate_up", "w_down", "prompt_k", "prompt_v")}
+        scales = {n: [] for n in ("wqkv", "wo", "w_gate_up", "w_down")}
         for l in range(L):
             g = lambda n: weights.torch(n, l).to(dev)     # noqa: E731
-            cols["wqkv"].append(pack_many([g("wq"), g("wk"), g("wv")], cfg.d_model))
-            cols["wo"].append(pack_many([g("wo")], cfg.n_heads * hd))
-            cols["w_gate_up"].append(pack_many([g("w_gate"), g("w_up")], cfg.d_model, interleave=True))
-            cols["w_down"].append(pack_many([g("w_down")], cfg.d_ffn))
+            for name, parts, k, interleave in (("wqkv", ("wq", "wk", "wv"), cfg.d_model, False), ("wo", ("wo",), cfg.n_heads * hd, False),
+                                               ("w_gate_up", ("w_gate", "w_up"), cfg.d_model, True), ("w_down", ("w_down",), cfg.d_ffn, False)):
+                parts = [g(p) for p in parts]
+                if int8:
+                    packed, scale = pack_many_q8(parts, k, interleave)
+                    scales[name].append(scale)
+                else:
+                    packed = pack_many(parts, k, interleave)
+                cols[name].append(packed)
             cols["attn_norm"].append(small("attn_norm", l))
             cols["ffn_norm"].append(small("ffn_norm", l))
             if cfg.n_prompt > 0:
@@ -235,7 +261,11 @@ class Model:
         torch.cuda.synchronize()
         self.max_pos = int(max_pos)
         self.handle = C.c_void_p()
-        _check(lib().bita_model_create(C.byref(c), C.byref(w), C.byref(self.handle)))
+        if int8:
+            sq = _ScalesQ8(**{n: arr(ts) for n, ts in scales.items()})
+            _check(lib().bita_model_create_q8(C.byref(c), C.byref(w), C.byref(sq), C.byref(self.handle)))
+        else:
+            _check(lib().bita_model_create(C.byref(c), C.byref(w), C.byref(self.handle)))
 
     def workspace_bytes(self, batch, rows):
         return lib().bita_workspace_bytes(self.handle, batch, rows)

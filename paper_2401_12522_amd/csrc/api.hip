@@ -93,6 +93,23 @@ extern "C" int bita_model_create(const bita_config *cfg, const bita_weights *w, 
     return BITA_OK;
 }
 
+extern "C" int bita_model_create_q8(const bita_config *cfg, const bita_weights *w, const bita_scales_q8 *sc, bita_model **out) {
+    if (!sc || !sc->wqkv || !sc->wo || !sc->w_gate_up || !sc->w_down) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_model_create_q8: missing scales");
+    if (cfg && (cfg->n_layers <= 0 || (int64_t)cfg->n_heads * cfg->head_dim > BITA_Q8_MAX_K || cfg->d_ffn > BITA_Q8_MAX_K))
+        return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_model_create_q8: attention width and d_ffn at most %d", BITA_Q8_MAX_K);
+    for (int l = 0; cfg && l < cfg->n_layers; l++)
+        if (!sc->wqkv[l] || !sc->wo[l] || !sc->w_gate_up[l] || !sc->w_down[l])
+            return bita_set_error(BITA_ERR_INVALID_ARG, "bita_model_create_q8: null scales in layer %d", l);
+    bita_model *m = nullptr;
+    if (int rc = bita_model_create(cfg, w, &m)) return rc;
+    m->s_qkv.assign(sc->wqkv, sc->wqkv + cfg->n_layers);
+    m->s_o.assign(sc->wo, sc->wo + cfg->n_layers);
+    m->s_gate_up.assign(sc->w_gate_up, sc->w_gate_up + cfg->n_layers);
+    m->s_down.assign(sc->w_down, sc->w_down + cfg->n_layers);
+    *out = m;
+    return BITA_OK;
+}
+
 extern "C" void bita_model_destroy(bita_model *m) {
     if (!m) return;
     if (m->rope_cos) (void)hipFree(m->rope_cos);
@@ -246,11 +263,14 @@ static void timed_gemm(const void *a_frag, int M, int64_t K, const void *w, int6
 // ------------------------------------------------------------------------------------------
 struct WsLayout {
     size_t x, h, q, attn_out, act, partial, part_o, part_ml, logits, ssq, kv_lo, total;
+    size_t codes, code_scale, sums, sums_bytes;         // 8-bit layers: a row's integers and scales, a split product's sums
     size_t partial_bytes;
 };
 #define ATTN_MAX_SPLITS 32
+static int64_t code_stride(int64_t k) { return (k + 15) / 16 * 16; }
 
-static WsLayout ws_layout(const bita_config &c, int batch, int rows) {
+static WsLayout ws_layout(const bita_model &m, int batch, int rows) {
+    const bita_config &c = m.cfg;
     const size_t M = (size_t)batch * rows;
     const int64_t nqkv = (int64_t)(c.n_heads + 2 * c.n_kv_heads) * c.head_dim, nq = (int64_t)c.n_heads * c.head_dim;
     WsLayout L;
@@ -260,15 +280,27 @@ static WsLayout ws_layout(const bita_config &c, int batch, int rows) {
     // GEMM inputs: two bf16 planes (hi, lo) in fragment order; queries: two row-major planes
     L.h = take(frag_bytes((int)M, c.d_model));
     L.q = take(2 * M * nq * 2);
-    L.attn_out = take(frag_bytes((int)M, nq));
-    L.act = take(frag_bytes((int)M, c.d_ffn));
+    L.attn_out = take(m.q8() ? M * nq * 2 : frag_bytes((int)M, nq));       // (8-bit layers: bf16 in rows)
+    L.act = take(m.q8() ? 0 : frag_bytes((int)M, c.d_ffn));
     size_t pb = 0;
-    const int64_t shapes[5][2] = {{nqkv, c.d_model}, {c.d_model, nq}, {2 * (int64_t)c.d_ffn, c.d_model},
-                                  {c.d_model, c.d_ffn}, {c.vocab, c.d_model}};
+    const int64_t shapes[5][2] = {{c.vocab, c.d_model}, {nqkv, c.d_model}, {c.d_model, nq}, {2 * (int64_t)c.d_ffn, c.d_model},
+                                  {c.d_model, c.d_ffn}};
+    L.sums_bytes = 0;
     for (auto &s : shapes) {
-        const GemmPlan p = gemm_plan((int)M, s[0], s[1]);
-        const size_t b = (size_t)p.splits * M * s[0] * 4;
+        const bool eight = m.q8() && &s != &shapes[0];                     // (the LM head stays bf16)
+        const size_t b = (size_t)(eight ? 1 : gemm_plan((int)M, s[0], s[1]).splits) * M * s[0] * 4;
         if (b > pb) pb = b;
+        if (eight) {
+            const size_t sums = bita_gemm_q8_workspace_bytes((int)M, s[0], s[1]);
+            if (sums > L.sums_bytes) L.sums_bytes = sums;
+        }
+    }
+    L.codes = L.code_scale = L.sums = off;
+    if (m.q8()) {
+        const int64_t widest = nq > c.d_ffn ? (nq > c.d_model ? nq : c.d_model) : (c.d_ffn > c.d_model ? c.d_ffn : c.d_model);
+        L.codes = take(M * code_stride(widest));
+        L.code_scale = take(M * 4);
+        L.sums = take(L.sums_bytes);
     }
     L.partial_bytes = pb;
     L.partial = take(pb);
@@ -302,7 +334,7 @@ int page_map_of(const bita_kv *kv, int ctx_upper, PageMap *pm, const char *who) 
 
 extern "C" size_t bita_workspace_bytes(const bita_model *m, int32_t batch, int32_t rows) {
     if (!m || batch <= 0 || rows <= 0) return 0;
-    return ws_layout(m->cfg, batch, rows).total;
+    return ws_layout(*m, batch, rows).total;
 }
 
 int verify_pass(bita_model *m, const bita_kv *kv, const bita_tree_template *t, const int32_t *d_token,
@@ -328,7 +360,7 @@ int verify_pass(bita_model *m, const bita_kv *kv, const bita_tree_template *t, c
     const int deepest = td.depth_max + td.n_mask;       // mask chains extend the depth by up to n
     if (kv->ctx_hint + deepest >= c.max_pos)
         return bita_set_error(BITA_ERR_CAPACITY, "bita_verify_step: position %d beyond rotary table (%d)", kv->ctx_hint + deepest, c.max_pos);
-    const WsLayout L = ws_layout(c, batch, td.rows);
+    const WsLayout L = ws_layout(*m, batch, td.rows);
     if (ws_bytes < L.total)
         return bita_set_error(BITA_ERR_CAPACITY, "bita_verify_step: workspace %zu < %zu bytes", ws_bytes, L.total);
     PageMap pm;
@@ -374,6 +406,30 @@ int verify_pass(bita_model *m, const bita_kv *kv, const bita_tree_template *t, c
         timed_gemm(actr, Mr, c.d_ffn, m->w_down[l], d, part, d, pdn, s);
         return pdn.splits;
     };
+    // The same with 8-bit layers: every product's rows are rounded in front of it (buffers of workspace layout W at wsr).
+    int rc8 = BITA_OK;
+    auto product_q8 = [&](int Mr, int64_t K, const void *w, const float *sw, int64_t N, float *to, unsigned char *wsr, const WsLayout &W) {
+        GemmRecord *r = (g_prof_on && g_prof_used < g_prof.size()) ? &g_prof[g_prof_used++] : nullptr;
+        if (r) { r->weight_bytes = N * K; (void)hipEventRecord(r->start, s); }
+        if (!rc8) rc8 = bita_gemm_q8((const int8_t *)(wsr + W.codes), code_stride(K), (const float *)(wsr + W.code_scale), Mr, K, w, sw, N,
+                                     wsr + W.sums, W.sums_bytes, to, BITA_F32, N, stream);
+        if (r) (void)hipEventRecord(r->stop, s);
+    };
+    auto norm_q8 = [&](int Mr, float *xr, const float *delta, const void *gain, unsigned char *wsr, const WsLayout &W) {
+        if (!rc8) rc8 = bita_norm_q8(xr, BITA_F32, Mr, d, d, delta, BITA_F32, d, gain, c.rms_eps, delta ? xr : nullptr, d, (int8_t *)(wsr + W.codes),
+                                     code_stride(d), (float *)(wsr + W.code_scale), stream);
+    };
+    auto after_attention_q8 = [&](int l, int Mr, const void *attn, float *xr, float *part, unsigned char *wsr, const WsLayout &W) {
+        int8_t *codes = (int8_t *)(wsr + W.codes);
+        float *scale = (float *)(wsr + W.code_scale);
+        if (!rc8) rc8 = bita_quantize_rows(attn, BITA_BF16, Mr, nq, nq, codes, code_stride(nq), scale, stream);
+        product_q8(Mr, nq, m->wo[l], m->s_o[l], d, part, wsr, W);
+        norm_q8(Mr, xr, part, m->ffn_norm[l], wsr, W);
+        product_q8(Mr, d, m->w_gate_up[l], m->s_gate_up[l], 2 * (int64_t)c.d_ffn, part, wsr, W);
+        if (!rc8) rc8 = bita_silu_mul_q8(part, BITA_F32, Mr, c.d_ffn, 2 * (int64_t)c.d_ffn, 16, codes, code_stride(c.d_ffn), scale, stream);
+        product_q8(Mr, c.d_ffn, m->w_down[l], m->s_down[l], d, part, wsr, W);
+        return 1;
+    };
     // Final norm, LM head and logits of Mr rows whose last FFN sums are still pending.
     auto head = [&](int Mr, int n_pending, float *xr, unsigned char *hr, float *part, float *ssqr, float *lg, const GemmPlan &plm) {
         const RowScale rs = {ssqr, (d / 4 + 255) / 256, 1.0f / (float)d, c.rms_eps};
@@ -393,10 +449,15 @@ int verify_pass(bita_model *m, const bita_kv *kv, const bita_tree_template *t, c
     int pending = 0;                                    // split-K partials waiting to be added to x
     for (int l = 0; l < c.n_layers; l++) {
         if (l == 0) launch_embed_prep(d_token, source, td, batch, m->tok_emb, m->mask_emb, d, c.vocab, m->attn_norm[0], x, h, ssq, s);
-        else launch_rmsnorm_prep(x, partial, pending, M, d, m->attn_norm[l], h, ssq, s);
+        else if (!m->q8()) launch_rmsnorm_prep(x, partial, pending, M, d, m->attn_norm[l], h, ssq, s);
+        if (m->q8()) norm_q8(M, x, l ? partial : nullptr, m->attn_norm[l], ws, L);
         void *kt = (unsigned char *)kv->k_tree + l * kv_layer_tree, *vt = (unsigned char *)kv->v_tree + l * kv_layer_tree;
         // with a single split the QKV product rotates and stores its columns itself
-        if (gemm_direct_output_possible(p_qkv, GEMM_OUT_ROPE)) {
+        if (m->q8()) {
+            product_q8(M, d, m->wqkv[l], m->s_qkv[l], nqkv, partial, ws, L);
+            launch_qkv_rope(partial, 1, batch, td, c.n_heads, c.n_kv_heads, hd, d_ctx_len, m->rope_cos, m->rope_sin, c.max_pos, q, q_lo, kt, vt, k_lo,
+                            v_lo, RowScale{nullptr, 0, 0.f, 0.f}, s);
+        } else if (gemm_direct_output_possible(p_qkv, GEMM_OUT_ROPE)) {
             const GemmOutput rotated = {GEMM_OUT_ROPE, rs_norm, nullptr, 0,
                                         {d_ctx_len, td.depth, m->rope_cos, m->rope_sin, (uint16_t *)q, (uint16_t *)q_lo, (uint16_t *)kt, (uint16_t *)vt,
                                          (uint16_t *)k_lo, (uint16_t *)v_lo, td.rows, c.n_heads, c.n_kv_heads, hd, c.max_pos}};
@@ -411,15 +472,17 @@ int verify_pass(bita_model *m, const bita_kv *kv, const bita_tree_template *t, c
         launch_tree_attention(td, q, q_lo, (unsigned char *)kv->k_cache + l * kv_layer_cache,
                               (unsigned char *)kv->v_cache + l * kv_layer_cache, kt, vt, k_lo, v_lo, m->prompt_k[l],
                               m->prompt_v[l], d_ctx_len, d_token, batch, c.n_heads, c.n_kv_heads, hd, c.n_prompt, kv->smax,
-                              ap, part_o, part_ml, attn_out, nullptr, true, pm, s, tail_layer ? tail->sel_row : nullptr);
+                              ap, part_o, part_ml, attn_out, nullptr, !m->q8(), pm, s, tail_layer ? tail->sel_row : nullptr);
         if (tail_layer) {
             // One row per sequence goes on: its attention output and residual are gathered, and the
             // rest of the layer, the LM head and the selection run on `batch` rows.
-            const WsLayout T = ws_layout(c, batch, 1);
+            const WsLayout T = ws_layout(*m, batch, 1);
             unsigned char *tw = (unsigned char *)tail->ws;
             float *tx = (float *)(tw + T.x), *tpart = (float *)(tw + T.partial), *tssq = (float *)(tw + T.ssq), *tlog = (float *)(tw + T.logits);
-            launch_gather_rows(tail->sel_row, batch, td.rows, attn_out, (int)nq, x, d, tw + T.attn_out, tx, s);
-            const int n_pending = after_attention(l, batch, tw + T.attn_out, tx, tw + T.h, tw + T.act, tpart, tssq, gemm_plan(batch, d, nq),
+            if (m->q8()) launch_gather_plain_rows(tail->sel_row, batch, td.rows, attn_out, (int)nq, x, d, tw + T.attn_out, tx, s);
+            else launch_gather_rows(tail->sel_row, batch, td.rows, attn_out, (int)nq, x, d, tw + T.attn_out, tx, s);
+            const int n_pending = m->q8() ? after_attention_q8(l, batch, tw + T.attn_out, tx, tpart, tw, T)
+                                          : after_attention(l, batch, tw + T.attn_out, tx, tw + T.h, tw + T.act, tpart, tssq, gemm_plan(batch, d, nq),
                                                   gemm_plan(batch, 2 * (int64_t)c.d_ffn, d), gemm_plan(batch, d, c.d_ffn));
             head(batch, n_pending, tx, tw + T.h, tpart, tssq, tlog, gemm_plan(batch, c.vocab, d));
             TemplateDev one = td;                        // one greedy row per sequence
@@ -428,8 +491,10 @@ int verify_pass(bita_model *m, const bita_kv *kv, const bita_tree_template *t, c
             launch_select(tlog, batch, one, c.vocab, 1, d_argmax, nullptr, nullptr, s);
             break;
         }
-        pending = after_attention(l, M, attn_out, x, h, act, partial, ssq, p_o, p_gu, p_dn);
+        pending = m->q8() ? after_attention_q8(l, M, attn_out, x, partial, ws, L) : after_attention(l, M, attn_out, x, h, act, partial, ssq, p_o, p_gu, p_dn);
+        if (rc8) return rc8;
     }
+    if (rc8) return rc8;
     if (tail) {
         BITA_HIP_CHECK(hipGetLastError());
         return BITA_OK;

@@ -102,6 +102,9 @@ struct bita_model {
     bita_config cfg;
     const void *tok_emb, *mask_emb, *final_norm, *lm_head;
     std::vector<const void *> attn_norm, ffn_norm, wqkv, wo, w_gate_up, w_down, prompt_k, prompt_v;
+    // a model with 8-bit layers (bita_model_create_q8): the scales of its four matrices' rows; empty otherwise
+    std::vector<const float *> s_qkv, s_o, s_gate_up, s_down;
+    bool q8() const { return !s_qkv.empty(); }
     float *rope_cos = nullptr, *rope_sin = nullptr;     // [max_pos][hd/2]
     // chain templates of the prefill chunks by row count, created once and kept until the
     // handle is destroyed (the enqueued kernels read their device arrays)
@@ -251,6 +254,9 @@ __device__ __forceinline__ int tree_token(const BuildSource &s, const TemplateDe
     return (g >= 0 && lvl >= 0 && lvl < t.n_mask && row < s.cand_rows && rank < s.kmax)
                ? s.cand[((int64_t)b * s.cand_rows + row) * s.kmax + rank] : -1;
 }
+// the same for a bf16 matrix in rows (8-bit layers): [batch * rows][k] and [batch * rows][d] -> [batch][k] and [batch][d]
+void launch_gather_plain_rows(const int32_t *sel_row, int batch, int rows, const void *a, int k, const float *x, int d, void *a_out,
+                              float *x_out, hipStream_t s);
 // row sel_row[b] of each sequence of `rows`: its columns of a two-plane slab (fragment order) and of
 // the residual stream, into a slab and a stream of `batch` rows
 void launch_gather_rows(const int32_t *sel_row, int batch, int rows, const void *a_frag, int k, const float *x, int d,

@@ -379,6 +379,21 @@ __global__ void gather_rows_kernel(const int32_t *__restrict__ sel_row, int rows
     if (i < (d >> 2)) reinterpret_cast<float4 *>(x_out + (int64_t)b * d)[i] = reinterpret_cast<const float4 *>(x + (int64_t)row * d)[i];
 }
 
+// The same out of a bf16 matrix in rows; k and d multiples of 4.
+__global__ void gather_plain_rows_kernel(const int32_t *__restrict__ sel_row, int rows, const uint2 *__restrict__ a, int k4, const float4 *__restrict__ x,
+                                         int d4, uint2 *__restrict__ a_out, float4 *__restrict__ x_out) {
+    const int b = blockIdx.x, i = blockIdx.y * blockDim.x + threadIdx.x;
+    const int64_t row = b * rows + min(max(sel_row[b], 0), rows - 1);
+    if (i < k4) a_out[(int64_t)b * k4 + i] = a[row * k4 + i];
+    if (i < d4) x_out[(int64_t)b * d4 + i] = x[row * d4 + i];
+}
+void launch_gather_plain_rows(const int32_t *sel_row, int batch, int rows, const void *a, int k, const float *x, int d, void *a_out,
+                              float *x_out, hipStream_t s) {
+    const int n = (k > d ? k : d) / 4;
+    hipLaunchKernelGGL(gather_plain_rows_kernel, dim3(batch, (n + 255) / 256), dim3(256), 0, s, sel_row, rows, (const uint2 *)a, k / 4, (const float4 *)x,
+                       d / 4, (uint2 *)a_out, (float4 *)x_out);
+}
+
 // ---------------------------------------------------------------------------------------
 void launch_gather_rows(const int32_t *sel_row, int batch, int rows, const void *a_frag, int k, const float *x, int d,
                         void *a_out, float *x_out, hipStream_t s) {

@@ -24,13 +24,14 @@ def main():
     ap.add_argument("--batch", type=int, default=1)
     ap.add_argument("--reps", type=int, default=3)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--int8", action="store_true", help="8-bit layers")
     args = ap.parse_args()
     B.lib()
     cfg = synth.get_config(args.workload)
     chunks = [int(c) for c in args.chunks.split(",")]
     smax = (args.ctx + 63) // 64 * 64
     w = synth.SynthWeights(cfg, seed=args.seed, device="cuda")
-    model = B.Model(cfg, w, max_pos=smax + 64, free_source=True)
+    model = B.Model(cfg, w, max_pos=smax + 64, free_source=True, int8=args.int8)
     kv = B.KVState(cfg, cfg.n_layers, args.batch, smax, max(chunks))
     toks = np.stack([synth.random_context(cfg.vocab, args.ctx, args.seed + 7919 * b) for b in range(args.batch)])
     toks = torch.tensor(toks, dtype=torch.int32, device="cuda")

@@ -55,3 +55,24 @@ def test_packed_sizes():
     assert L.bita_packed_q8_bytes(32, 688) == 2 * 6 * 2048
     assert L.bita_packed_q8_bytes(33, 1) == 3 * 2048
     assert L.bita_packed_q8_bytes(0, 5) == L.bita_packed_q8_bytes(5, 0) == 0
+
+
+def test_refusals_of_an_8_bit_model():
+    import ctypes as C
+    import paper_2401_12522_amd as bita
+    L = bita.lib()
+    cfg = bita.binding._Config(1, 64, 1, 1, 64, 16, 16, 0, 0, 8, 1e-5, 1e4)
+    w, sq, handle = bita.binding._Weights(), bita.binding._ScalesQ8(), C.c_void_p()
+    assert L.bita_model_create_q8(C.byref(cfg), C.byref(w), None, C.byref(handle)) == -1
+    assert L.bita_model_create_q8(C.byref(cfg), C.byref(w), C.byref(sq), C.byref(handle)) == -1
+    one = (C.c_void_p * 1)(1 << 20)
+    none = (C.c_void_p * 1)(None)
+    for n in ("wqkv", "wo", "w_gate_up", "w_down"):
+        setattr(sq, n, one)
+    sq.wo = none
+    assert L.bita_model_create_q8(C.byref(cfg), C.byref(w), C.byref(sq), C.byref(handle)) == -1
+    sq.wo = one
+    assert L.bita_model_create_q8(C.byref(cfg), C.byref(w), C.byref(sq), C.byref(handle)) == -1         # (no weights)
+    wide = bita.binding._Config(1, 64, 1, 1, 64, 131072, 16, 0, 0, 8, 1e-5, 1e4)
+    assert L.bita_model_create_q8(C.byref(wide), C.byref(w), C.byref(sq), C.byref(handle)) == -4
+    assert not handle
