@@ -374,8 +374,9 @@ int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t
  * of bita_weights, and the fp32 scales of their rows in the same order (gate/up: tiles of 16 in turn).  Everything else is as for
  * bita_model_create: embeddings, norms, prompt prefix and LM head in bf16, the K/V cache too.  Every call that takes a
  * model takes this one; each layer runs bita_norm_q8, bita_gemm_q8, attention, bita_quantize_rows (the attention output as bf16),
- * bita_gemm_q8, bita_norm_q8, bita_gemm_q8, bita_silu_mul_q8 and bita_gemm_q8.  A row's integers are its own, so drafted and plain
- * decoding see the same model.  n_heads * head_dim and d_ffn at most BITA_Q8_MAX_K.  The members are HOST arrays of n_layers device pointers. */
+ * bita_gemm_q8, bita_norm_q8, bita_gemm_q8, bita_silu_mul_q8 and bita_gemm_q8.  A row's integers and products are its own, whatever
+ * other rows a pass has; attention's last bits, which may differ between passes of different row counts, can take a value across a
+ * rounding border, so that drafted and plain decoding agree up to tokens as near to each other as that changes.  n_heads * head_dim and d_ffn at most BITA_Q8_MAX_K.  The members are HOST arrays of n_layers device pointers. */
 typedef struct bita_scales_q8 {
     const float *const *wqkv, *const *wo, *const *w_gate_up, *const *w_down;
 } bita_scales_q8;

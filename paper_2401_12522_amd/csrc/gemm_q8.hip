@@ -48,12 +48,48 @@ __device__ __forceinline__ void store4(void *out, int out_type, int64_t ldo, int
     } else {
         uint16_t *p = (uint16_t *)out + (int64_t)row * ldo + col, h[4];
 #pragma unroll
-        for (int e = 0; e < 4; e++) h[e] = v[e] != v[e] ? (uint16_t)0x7FC0 : f32_to_bf16(v[e]);
+        for (int e = 0; e < 4; e++) h[e] = __builtin_bit_cast(uint16_t, (__bf16)v[e]);
         if (col + 4 <= n) *reinterpret_cast<Halves4 *>(p) = Halves4{{h[0], h[1], h[2], h[3]}};
         else
             for (int e = 0; e < 3; e++)
                 if (col + e < n) p[e] = h[e];
     }
+}
+
+// V neighbouring columns of one row (16 bytes), with their scales
+struct __attribute__((packed, aligned(2))) Halves8 { uint32_t w[4]; };
+template <int V>
+__device__ __forceinline__ void store_row(float *out, int64_t ldo, int row, int64_t col, int64_t n, const int sum[V], float sa, const float scale[V]) {
+    float *p = out + (int64_t)row * ldo + col, v[V];
+#pragma unroll
+    for (int e = 0; e < V; e++) v[e] = (float)sum[e] * sa * scale[e];
+    if (col + V <= n) {
+        *reinterpret_cast<Words4 *>(p) = Words4{{v[0], v[1], v[2], v[3]}};
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < V; e++)
+        if (col + e < n) p[e] = v[e];
+}
+template <int V>
+__device__ __forceinline__ void store_row(int *out, int64_t ldo, int row, int64_t col, int64_t, const int sum[V], float, const float *) {      // (whole tiles: no end inside)
+    *reinterpret_cast<i32x4 *>(out + (int64_t)row * ldo + col) = i32x4{sum[0], sum[1], sum[2], sum[3]};
+}
+template <int V>
+__device__ __forceinline__ void store_row(uint16_t *out, int64_t ldo, int row, int64_t col, int64_t n, const int sum[V], float sa, const float scale[V]) {
+    uint16_t *p = out + (int64_t)row * ldo + col, h[V];
+#pragma unroll
+    for (int e = 0; e < V; e++) h[e] = __builtin_bit_cast(uint16_t, (__bf16)((float)sum[e] * sa * scale[e]));
+    if (col + V <= n) {
+        Halves8 q;
+#pragma unroll
+        for (int e = 0; e < V / 2; e++) q.w[e] = h[2 * e] | (uint32_t)h[2 * e + 1] << 16;
+        *reinterpret_cast<Halves8 *>(p) = q;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < V; e++)
+        if (col + e < n) p[e] = h[e];
 }
 
 // Few rows, one pass over the weights.  A workgroup has MT tiles of 16 rows and WN of 16 columns; KG groups of WN waves share the
@@ -69,14 +105,12 @@ template <int MT, int WN, int KG, int P>
 __global__ __launch_bounds__(WN * KG * 64) void gemm_q8_skinny_kernel(const int8_t *__restrict__ a, int64_t lda, const i32x4 *__restrict__ w, int m, int k_steps,
                                                              int k16, int64_t n, const float *__restrict__ sa, const float *__restrict__ sw,
                                                              void *__restrict__ out, int64_t ldo, int out_type, int split_steps, int *__restrict__ part) {
-    constexpr int SK = 8, WAVES = WN * KG, SW = SK / KG, ROWS = 16 * MT, PIECES = 4 * SK, LR = 64 / PIECES, STAGE = ROWS * PIECES, NL = STAGE / 64, AL = (NL + WAVES - 1) / WAVES;      // loads of a stage, of a wave
-    static_assert(SK % KG == 0, "whole k-steps");
-    constexpr int SWZ = PIECES < 16 ? PIECES - 1 : 15;       // waves along N, k-steps of a wave in a stage; 16-byte pieces
-    extern __shared__ __attribute__((aligned(16))) i32x4 lds[];                  // [2][ROWS][32], then [KG][MT * NW * WN][64]
+    constexpr int SK = 8, WAVES = WN * KG, SW = SK / KG;                         // k-steps of a stage, of a wave in it
+    constexpr int ROWS = 16 * MT, STAGE = ROWS * 32, NL = STAGE / 64, AL = (NL + WAVES - 1) / WAVES;   // 16-byte pieces of a stage; its loads, a wave's
+    extern __shared__ __attribute__((aligned(16))) i32x4 lds[];                  // [2][ROWS][32], then [KG][MT * WN][64]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = wave / WN, wn = wave % WN, r = lane & 15, c = lane >> 4;
     const int64_t n_tiles = (n + 15) >> 4, tile = (int64_t)blockIdx.x * WN + wn;
     const int m0 = blockIdx.y * ROWS, first = blockIdx.z * split_steps, last = min(k_steps, first + split_steps), stages = (last - first + SK - 1) / SK;
-    // staging: a load of 2 rows x 512 bytes; piece p of row x lies at p ^ (x % 16), so that 16 rows of one piece are 16 different bank groups
     // (offsets out of the descriptor's range read zeros and move nothing: rows and columns past the end, stages past the last)
     constexpr uint32_t NOWHERE = 0xFFFFFFF0u;
     const int8_t *ab = a + (int64_t)m0 * lda;
@@ -86,9 +120,9 @@ __global__ __launch_bounds__(WN * KG * 64) void gemm_q8_skinny_kernel(const int8
     int piece[AL];
 #pragma unroll
     for (int i = 0; i < AL; i++) {
-        const int x = LR * (i * WAVES + wave) + lane / PIECES;
+        const int x = 2 * (i * WAVES + wave) + (lane >> 5);
         a_row[i] = x < rows ? (uint32_t)(x * lda) : NOWHERE;                 // (loads past the last row of the tile: none)
-        piece[i] = ((lane % PIECES) ^ (x & SWZ)) * 16;
+        piece[i] = ((lane & 31) ^ (x & 15)) * 16;
     }
     const i32x4 *wt = w + min(tile, n_tiles - 1) * 128;
     const uint32_t w_bytes = tile < n_tiles ? 2048 : 0;
@@ -108,9 +142,9 @@ __global__ __launch_bounds__(WN * KG * 64) void gemm_q8_skinny_kernel(const int8
     };
     i32x4 fa[2][MT];
     auto read_a = [&](int buf, int s) __attribute__((always_inline)) {
-        const int at = buf * STAGE + r * PIECES + (((kg * SW + s) * 4 + c) ^ (r & SWZ));
+        const int at = buf * STAGE + r * 32 + (((kg * SW + s) * 4 + c) ^ r);
 #pragma unroll
-        for (int i = 0; i < MT; i++) fa[s & 1][i] = lds[at + i * 16 * PIECES];
+        for (int i = 0; i < MT; i++) fa[s & 1][i] = lds[at + i * 512];
     };
     auto put_a = [&](int buf, int set) __attribute__((always_inline)) {
 #pragma unroll
@@ -184,39 +218,34 @@ __global__ __launch_bounds__(WN * KG * 64) void gemm_q8_skinny_kernel(const int8
     }
 }
 
-// Sums of the k splits, scaled and stored: a thread has four columns of a row.
-__global__ __launch_bounds__(256) void gemm_q8_reduce_kernel(const int *__restrict__ part, int splits, int m, int64_t n, const float *__restrict__ sa,
+// Sums of the k splits, scaled and stored: a thread has four columns of a row (ld4: a row's groups of four).
+__global__ __launch_bounds__(256) void gemm_q8_reduce_kernel(const i32x4 *__restrict__ part, int splits, int m, int64_t n, uint32_t ld4, const float *__restrict__ sa,
                                                              const float *__restrict__ sw, void *__restrict__ out, int64_t ldo, int out_type) {
-    const int64_t ld = (n + 15) / 16 * 16, col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    const int row = blockIdx.y;
-    if (col >= n) return;
-    const i32x4 *p = reinterpret_cast<const i32x4 *>(part + (int64_t)row * ld + col);
-    const int64_t step = (int64_t)m * ld / 4;
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, row = at / ld4, col = (at - row * ld4) * 4;
+    if (row >= (uint32_t)m || col >= n) return;
+    const int64_t step = (int64_t)m * ld4;
     i32x4 q[8], sum = {0, 0, 0, 0};
-    for (int s0 = 0; s0 < splits; s0 += 8) {                                 // (requested together; those past the last are left out)
 #pragma unroll
-        for (int s = 0; s < 8; s++) q[s] = p[min(s0 + s, splits - 1) * step];
+    for (int s = 0; s < 8; s++) q[s] = part[at + min(s, splits - 1) * step];      // (requested together; those past the last are left out)
 #pragma unroll
-        for (int s = 0; s < 8; s++)
-            if (s0 + s < splits) sum += q[s];
-    }
+    for (int s = 0; s < 8; s++)
+        if (s < splits) sum += q[s];
     store4(out, out_type, ldo, row, col, n, sum, sa[row], sw);
 }
 
 // Many rows: tiles of 32 MF WM rows and 32 NF WN columns, WM x WN waves of MF x NF matrix tiles of 32 x 32 each, both operands
 // through two LDS buffers of 128 k: rows of 128 bytes with piece p of row x at p ^ (x % 8), weight blocks as they are packed (the
 // stage's are one run of memory).  Each stage's loads are spread over its matrix instructions, two stages ahead of their use.
-// What bounds 256 x 256 tiles (4096 rows x 57344 x 8192, 1.87 ms, 2060 TOP/s): the matrix instructions alone take 1.30 ms (at the
-// clock that the card holds under them; 2400 TOP/s is what the library's 8192^3 reaches), LDS reads 0.19 more, LDS writes 0.13, loads
-// 0.25.  Weights straight to the registers of the WM waves that use them: 1.90 ms; four waves of 128 x 128: 2.01.
+// What bounds 256 x 256 tiles (4096 rows x 57344 x 8192, 1.76 ms, 2190 TOP/s; the library's 8192^3 2400): the matrix instructions
+// and the stores take 1.30 ms (at the clock that the card holds under them), LDS reads 0.19 more, LDS writes 0.13, loads 0.25.  Weights
+// straight to the registers of the WM waves that use them: 1.90 ms against 1.85 at the time; four waves of 128 x 128: 2.01.
 template <int MF, int NF, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
     const int8_t *__restrict__ a, int64_t lda, const i32x4 *__restrict__ w, int m, int k_pairs, int k16, int64_t n, int m_blocks, int n_blocks,
-    const float *__restrict__ sa, const float *__restrict__ sw, void *__restrict__ out, int64_t ldo, int out_type) {
+    const float *__restrict__ sa, const float *__restrict__ sw, void *__restrict__ out, int64_t ldo, int out_type, int split_pairs, int *__restrict__ part) {
     typedef __attribute__((ext_vector_type(16))) int i32x16;
     constexpr int WAVES = WM * WN, BM = 32 * MF * WM, AW = (BM / 8 + WAVES - 1) / WAVES;           // loads of 8 rows x 128 bytes, of a wave
     constexpr int BN = 32 * NF * WN, BW = (BN / 8 + WAVES - 1) / WAVES, LW = AW + BW;              // 1 KiB loads of weights, of a wave; of both
-    
     extern __shared__ __attribute__((aligned(16))) i32x4 lds[];                      // [2][BM rows: [piece ^ row % 8] | BN / 16 blocks of 2 KiB]
     constexpr int STAGE = (BM + BN) * 8;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
@@ -226,7 +255,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
     if (id >= total || (int)(blockIdx.x >> 3) >= per_xcd) return;
     const int group = id / (8 * n_blocks), in_group = id - group * 8 * n_blocks, tall = min(8, m_blocks - group * 8);
     const int nb = in_group / tall, mb = group * 8 + in_group - nb * tall;
-    const int m0 = mb * BM;
+    const int m0 = mb * BM, first = blockIdx.y * split_pairs, pairs = min(k_pairs - first, split_pairs), k_end = min(k16, (first + pairs) * 128);
     const int64_t n_tiles = (n + 15) >> 4, tile0 = (int64_t)nb * (BN / 16) + wn * 2 * NF;
     // (offsets out of the descriptor's range read zeros and move nothing)
     constexpr uint32_t NOWHERE = 0xFFFFFFF0u;
@@ -248,10 +277,10 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
     // the loads of a stage, one by one: the wave's rows of activations, then its pieces of the stage's weight blocks (one run of memory)
     auto fetch = [&](int i, int t) __attribute__((always_inline)) {
         if (i < AW) {
-            const int col = t * 128;
-            st[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, col + piece < k16 && a_row[i < AW ? i : 0] != NOWHERE ? a_row[i < AW ? i : 0] + col : NOWHERE, 0, 0));
+            const int col = (first + t) * 128;
+            st[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(a_rsrc, col + piece < k_end && a_row[i < AW ? i : 0] != NOWHERE ? a_row[i < AW ? i : 0] + col : NOWHERE, 0, 0));
         } else {
-            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(wt + (int64_t)t * n_tiles * 128), 0, t < k_pairs ? w_bytes : 0, 0x00027000);
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(wt + (int64_t)(first + t) * n_tiles * 128), 0, t < pairs ? w_bytes : 0, 0x00027000);
             st[i] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (i - AW) * WAVES + wave < BN / 8 ? ((i - AW) * WAVES + wave) * 1024 + lane * 16 : NOWHERE, 0, 0));
         }
     };
@@ -286,13 +315,13 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
     }
     __builtin_amdgcn_sched_barrier(0);
     barrier();
-    for (int t = 0; t < k_pairs; t++) {
+    for (int t = 0; t < pairs; t++) {
         const int buf = t & 1;
         read(buf, 0);
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             if (q < 3) read(buf, q + 1);
-            // a quarter of the next stage goes to the other buffer (read before the last barrier), and the one after it is asked for
+            // a third of the next stage goes to the other buffer (read before the last barrier), and the one after it is asked for
             if (q > 0) {
 #pragma unroll
                 for (int i = (q - 1) * LW / 3; i < q * LW / 3; i++) {
@@ -309,21 +338,44 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
         }
         barrier();
     }
-    // lane l of a tile's sums: row l % 32, value e at column 8 (e / 4) + 4 (l / 32) + e % 4
+    // Sums leave as whole row segments: lane l of a tile has row l % 32 and, as value e, column 8 (e / 4) + 4 (l / 32) + e % 4, 16 bytes of each of
+    // 32 rows a store; so a wave turns 32 rows at a time in LDS of its own (16 bytes more a row: rows start in different banks).  Straight from the
+    // registers 4096 rows of 22016 x 4096 in bf16 took 100 us longer than without stores.
+    constexpr int COLS = 32 * NF, LD = COLS / 4 + 1;                                  // in 16-byte pieces
+    static_assert(WAVES * 32 * LD <= 2 * STAGE, "the epilogue's rows fit the stages");
+    i32x4 *own = lds + wave * 32 * LD;
+    auto leave = [&](auto *o, int64_t ldo, int64_t n) __attribute__((always_inline)) {
+        constexpr int V = 16 / (int)sizeof(*o), LANES = COLS / V, ROWS = 64 / LANES;  // columns of a lane, lanes of a row, rows a store
+        const int c = lane % LANES;
+        const int64_t col = tile0 * 16 + c * V;
+        float scale[V];
 #pragma unroll
-    for (int i = 0; i < MF; i++) {
-        const int row = m0 + (wm * MF + i) * 32 + r;
-        if (row >= m) continue;
-        const float s = sa[row];
+        for (int e = 0; e < V; e++) scale[e] = !part && col + e < n ? sw[col + e] : 0.f;
 #pragma unroll
-        for (int j = 0; j < NF; j++)
+        for (int i = 0; i < MF; i++) {
+            const int first = m0 + (wm * MF + i) * 32;
+            if (first >= m) break;
 #pragma unroll
-            for (int e = 0; e < 4; e++) {
-                const int64_t col = (tile0 + 2 * j) * 16 + 8 * e + 4 * half;
-                const i32x4 v = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
-                if (col < n) store4(out, out_type, ldo, row, col, n, v, s, sw);
+            for (int j = 0; j < NF; j++)
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    own[r * LD + j * 8 + 2 * e + half] = i32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+#pragma unroll
+            for (int x = 0; x < 32; x += ROWS) {
+                const int in = x + lane / LANES, row = first + in;
+                int sum[V];
+#pragma unroll
+                for (int e = 0; e < V / 4; e++) {
+                    const i32x4 q = own[in * LD + c * (V / 4) + e];
+                    sum[4 * e] = q[0]; sum[4 * e + 1] = q[1]; sum[4 * e + 2] = q[2]; sum[4 * e + 3] = q[3];
+                }
+                if (row < m && col < n) store_row<V>(o, ldo, row, col, n, sum, sa[row], scale);
             }
-    }
+        }
+    };
+    if (part) leave(part + (int64_t)blockIdx.y * m * n_tiles * 16, n_tiles * 16, n_tiles * 16);
+    else if (out_type == BITA_F32) leave((float *)out, ldo, n);
+    else leave((uint16_t *)out, ldo, n);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -332,13 +384,13 @@ struct GemmQ8 {
     void *out; int out_type; int64_t ldo; int *part; hipStream_t s;
 };
 // How a product is cut.  form < SKINNY: a tile kernel; else weight tiles side by side in a workgroup of the skinny kernel, whose
-// workgroups have mt row tiles each; splits of k, of split_steps k-steps each.
+// workgroups have mt row tiles each; splits of k (at most 8), of split_steps k-steps each.
 enum { SKINNY = 16 };
 struct PlanQ8 { int form, mt, splits, split_steps; };
 
 // Tile kernels: rows and columns of a workgroup, and the time of 128 k of one, us (1024 rows x 4096 x 4096 in one round)
 struct TileForm { int rows, cols; float stage; };
-static const TileForm TILE_FORMS[] = {{256, 256, 2.06f}, {160, 256, 1.53f}, {128, 256, 1.16f}, {128, 128, 0.82f}, {64, 256, 0.87f}, {96, 192, 0.90f}};
+static const TileForm TILE_FORMS[] = {{256, 256, 2.06f}, {160, 256, 1.53f}, {128, 256, 1.16f}, {128, 128, 0.82f}, {96, 192, 0.90f}};
 static const int SKINNY_WIDE[] = {1, 2, 3, 4, 6, 8};
 #define SKINNY_MAX_MT 9
 
@@ -353,12 +405,18 @@ static PlanQ8 plan_q8(int m, int64_t n, int k_pairs) {
     const int stages = (k_pairs + 3) / 4;
     PlanQ8 best = {0, 0, 1, 2 * k_pairs};
     double best_us = 1e30;
-    for (int f = 0; f < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); f++) {
-        const TileForm &t = TILE_FORMS[f];
-        const double tiles = (double)(((int64_t)m + t.rows - 1) / t.rows) * (double)((n + t.cols - 1) / t.cols), rounds = ceil(tiles / 256);
-        const double us = 5 + rounds * k_pairs * t.stage;
-        if (us < best_us) { best_us = us; best = {f, 0, 1, 2 * k_pairs}; }
-    }
+    const double weights_us = 2048.0 * n_tiles * k_pairs / 6.3e6;
+    const auto sums_us = [&](int splits) { return splits > 1 ? 3 + 8.0 * splits * m * (16.0 * n_tiles) / 4.5e6 : 0.0; };
+    for (int f = 0; f < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); f++)
+        for (int splits = 1; splits <= 8 && (splits == 1 || splits * 8 <= k_pairs); splits++) {
+            const TileForm &t = TILE_FORMS[f];
+            const int per = (k_pairs + splits - 1) / splits;
+            if ((k_pairs + per - 1) / per != splits) continue;
+            const double tiles = (double)(((int64_t)m + t.rows - 1) / t.rows) * (double)((n + t.cols - 1) / t.cols);
+            if (splits > 1 && tiles * splits > 512) break;                      // (enough workgroups as it is)
+            const double us = 5 + fmax(ceil(tiles * splits / 256) * per * t.stage, weights_us) + sums_us(splits);
+            if (us < best_us) { best_us = us; best = {f, 0, splits, 2 * per}; }
+        }
     if (m > 2 * SKINNY_MAX_MT * 16) return best;
     const int mt_all = (m + 15) / 16, blocks = (mt_all + SKINNY_MAX_MT - 1) / SKINNY_MAX_MT, mt = (mt_all + blocks - 1) / blocks;
     for (int wide : SKINNY_WIDE) {
@@ -369,8 +427,8 @@ static PlanQ8 plan_q8(int m, int64_t n, int k_pairs) {
             const double groups = (double)((n_tiles + wide - 1) / wide) * blocks * splits, rounds = ceil(groups / 256);
             const double bytes = 512.0 * ((m + blocks - 1) / blocks + 16 * wide);
             const double stage = fmax(0.34, bytes / 52e3 * (mt > 5 ? 1.5 : 1.0));
-            double us = 2 + 1.5 * rounds + fmax(rounds * per * stage, 2048.0 * n_tiles * k_pairs / 6.3e6);
-            if (splits > 1) us += 3 + 8.0 * splits * m * (16.0 * n_tiles) / 4.5e6;
+            double us = 2 + 1.5 * rounds + fmax(rounds * per * stage, weights_us);
+            us += sums_us(splits);
             if (us < best_us) { best_us = us; best = {SKINNY + wide, mt, splits, 8 * per}; }
         }
     }
@@ -396,18 +454,20 @@ static void launch_skinny(const GemmQ8 &g, const PlanQ8 &p) {
     hipLaunchKernelGGL((gemm_q8_skinny_kernel<MT, WN, KG, P>), dim3((unsigned)((tiles + WN - 1) / WN), (unsigned)((g.m + 16 * MT - 1) / (16 * MT)), p.splits),
                        dim3(WN * KG * 64), SMEM, g.s, g.a, g.lda, g.w, g.m, 2 * g.k_pairs, g.k16, g.n, g.sa, g.sw, g.out, g.ldo, g.out_type, p.split_steps,
                        p.splits > 1 ? g.part : nullptr);
-    if (p.splits > 1)
-        hipLaunchKernelGGL(gemm_q8_reduce_kernel, dim3((unsigned)((g.n + 1023) / 1024), g.m), dim3(256), 0, g.s, g.part, p.splits, g.m, g.n, g.sa, g.sw, g.out,
-                           g.ldo, g.out_type);
+}
+static void launch_reduce(const GemmQ8 &g, const PlanQ8 &p) {
+    const uint32_t ld4 = (uint32_t)((g.n + 15) / 16 * 4);
+    hipLaunchKernelGGL(gemm_q8_reduce_kernel, dim3((unsigned)(((uint64_t)g.m * ld4 + 255) / 256)), dim3(256), 0, g.s, (const i32x4 *)g.part, p.splits, g.m, g.n,
+                       ld4, g.sa, g.sw, g.out, g.ldo, g.out_type);
 }
 template <int MF, int NF, int WM, int WN>
-static void launch_tile(const GemmQ8 &g) {
+static void launch_tile(const GemmQ8 &g, const PlanQ8 &p) {
     constexpr int BM = 32 * MF * WM, BN = 32 * NF * WN, SMEM = 2 * (BM + BN) * 128;
     const int m_blocks = (int)(((int64_t)g.m + BM - 1) / BM), n_blocks = (int)((g.n + BN - 1) / BN), total = m_blocks * n_blocks;
     static LdsLimit limit;
     raise_lds_limit(limit, (const void *)gemm_q8_tile_kernel<MF, NF, WM, WN>, SMEM);
-    hipLaunchKernelGGL((gemm_q8_tile_kernel<MF, NF, WM, WN>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(WM * WN * 64), SMEM, g.s, g.a, g.lda, g.w, g.m,
-                       g.k_pairs, g.k16, g.n, m_blocks, n_blocks, g.sa, g.sw, g.out, g.ldo, g.out_type);
+    hipLaunchKernelGGL((gemm_q8_tile_kernel<MF, NF, WM, WN>), dim3((unsigned)((total + 7) / 8 * 8), p.splits), dim3(WM * WN * 64), SMEM, g.s, g.a, g.lda, g.w, g.m,
+                       g.k_pairs, g.k16, g.n, m_blocks, n_blocks, g.sa, g.sw, g.out, g.ldo, g.out_type, p.split_steps / 2, p.splits > 1 ? g.part : nullptr);
 }
 // waves that share k where a workgroup has few columns; k two stages ahead where a stage is short
 template <int MT>
@@ -424,12 +484,11 @@ static void launch_skinny_mt(const GemmQ8 &g, const PlanQ8 &p) {
 static void launch_gemm_q8(const GemmQ8 &g, const PlanQ8 &p) {
     if (p.form < SKINNY) {
         switch (p.form) {
-            case 0: return launch_tile<4, 2, 2, 4>(g);
-            case 1: return launch_tile<5, 1, 1, 8>(g);
-            case 2: return launch_tile<2, 2, 2, 4>(g);
-            case 3: return launch_tile<2, 1, 2, 4>(g);
-            case 4: return launch_tile<2, 1, 1, 8>(g);
-            default: return launch_tile<3, 1, 1, 6>(g);
+            case 0: return launch_tile<4, 2, 2, 4>(g, p);
+            case 1: return launch_tile<5, 1, 1, 8>(g, p);
+            case 2: return launch_tile<2, 2, 2, 4>(g, p);
+            case 3: return launch_tile<2, 1, 2, 4>(g, p);
+            default: return launch_tile<3, 1, 1, 6>(g, p);
         }
     }
     switch (p.mt) {
@@ -500,7 +559,9 @@ extern "C" int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_sca
     const size_t need = plan_bytes(p, m_rows, n_rows);
     if (need && (!d_ws || ws_bytes < need || (uintptr_t)d_ws % 16))
         return bita_set_error(BITA_ERR_CAPACITY, "bita_gemm_q8: workspace %zu < %zu bytes, or not a multiple of 16", d_ws ? ws_bytes : (size_t)0, need);
-    launch_gemm_q8(GemmQ8{d_a, lda, d_a_scale, m_rows, k_pairs, k16, (const i32x4 *)d_w_packed, d_w_scale, n_rows, d_out, out_type, ldo, (int *)d_ws, (hipStream_t)stream}, p);
+    const GemmQ8 g = {d_a, lda, d_a_scale, m_rows, k_pairs, k16, (const i32x4 *)d_w_packed, d_w_scale, n_rows, d_out, out_type, ldo, (int *)d_ws, (hipStream_t)stream};
+    launch_gemm_q8(g, p);
+    if (p.splits > 1) launch_reduce(g, p);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
 }

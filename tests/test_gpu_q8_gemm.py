@@ -46,6 +46,28 @@ def test_product(m, n, k, dtype):
     check(y, a, sa, w, sw)
 
 
+@pytest.mark.parametrize("m,n,k,rows,cols,splits", [
+    # every workgroup shape, k whole and split, ragged at every end
+    (3, 64, 28672, 16, 16, 8), (16, 200, 9000, 16, 16, 4), (1, 4165, 107515, 16, 32, 1), (39, 8303, 10455, 48, 48, 1), (34, 3166, 21811, 48, 64, 4), (50, 28702, 2, 64, 128, 1),
+    (68, 1037, 11000, 80, 32, 5), (83, 3006, 23350, 96, 96, 8), (86, 916, 119981, 96, 32, 8), (109, 32758, 374, 112, 128, 1), (117, 1504, 61018, 128, 48, 8), (144, 22016, 300, 144, 128, 1),
+    (275, 4021, 189, 144, 32, 1), (160, 48, 131071, 80, 16, 8), (79, 79711, 905, 96, 192, 1), (144, 500, 9001, 128, 128, 8), (700, 300, 20000, 128, 128, 8),
+    (300, 100, 131071, 128, 128, 8), (1500, 130, 4001, 128, 128, 4), (149, 34781, 21400, 160, 256, 3), (293, 32003, 400, 160, 256, 1), (520, 9000, 400, 128, 256, 1),
+    (898, 12646, 1507, 256, 256, 1)])
+def test_workgroup_shapes(m, n, k, rows, cols, splits):
+    import paper_2401_12522_amd as bita
+    plan = bita.binding.gemm_q8_plan_info(m, n, k)
+    assert (plan["rows"], plan["cols"], plan["splits"]) == (rows, cols, splits), plan
+    (a, sa), (w, sw) = codes(m, k, 1), codes(n, k, 2)
+    need = bita.lib().bita_gemm_q8_workspace_bytes(m, n, k)
+    assert need == (splits * m * ((n + 15) // 16 * 16) * 4 if splits > 1 else 0)
+    packed, ws = bita.pack_weight_q8(w), torch.full((need + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((m, n), float("nan"), dtype=dtype, device="cuda")
+        bita.gemm_q8(a, sa, packed, sw, n, out=out, workspace=ws)
+        check(out, a, sa, w, sw)
+    assert bool((ws[need:] == 0xA5).all())
+
+
 def test_longest_sums():
     """The largest sums there are: all -128 over the longest k."""
     import paper_2401_12522_amd as bita
