@@ -10,10 +10,11 @@
 // the border (k + 1/2) a / 127 is whether 254 |v| - (2k + 1) a is positive, zero or negative, both terms exact in a double.
 //
 // One workgroup per row, whose values v it holds in registers as fp32: one pass over memory, one barrier for the row's maximum and sum
-// (the norm's and the gating's maximum is refined in double behind a second one: by the few threads that hold a candidate).  What bounds it is memory where there are many rows, provided
-// that a value costs few instructions and a row few waits: values in groups of eight a thread, one branch a group for all that is
-// rare, the waves' maxima and sums read side by side (one after the other they cost more than the row: 11008 rows of 4096 bf16
-// 91 us).
+// (the norm's and the gating's maximum is refined in double behind a second one: by the few threads that hold a candidate, who read
+// its sources again; held in registers they made the few rows no faster and the gating spill).  What bounds it is memory where there
+// are many rows, provided that a value costs few instructions and a row few waits: values in groups of eight a thread, one branch a
+// group for all that is rare, the waves' maxima and sums read side by side (one after the other they cost more than the row: 11008
+// rows of 4096 bf16 91 us).
 #include "common.h"
 
 enum { ROWS_PLAIN = 0, ROWS_NORM = 1, ROWS_GATE = 2 };
@@ -104,15 +105,29 @@ __device__ __forceinline__ float gated(float g, float u) {
 }
 __device__ __forceinline__ double gated_exactly(float g, float u) { return (double)g / (1.0 + exp(-(double)g)) * (double)u; }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-    return v;
+// Maximum and sum over a wave or its first 16 lanes, the same in every lane: moves between lanes inside the vector unit (zero from
+// outside: the values are >= 0), four shifts within 16 lanes and for a wave two broadcasts of 16 lanes' last, then one lane is read.
+// Moves through LDS cost more: 68 plain rows of 4096 bf16 4.0 us (these: 3.65), norm of 68 rows of 8192 fp32 8.0 (7.4), 68 gated rows of
+// 11008 fp32 8.0 (7.6), 11008 plain rows of 4096 bf16 29.5 (28.1).
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false); }
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+    const uint64_t w = (uint64_t)__double_as_longlong(v);
+    return __longlong_as_double((long long)((uint64_t)moved<CTRL>((uint32_t)(w >> 32)) << 32 | moved<CTRL>((uint32_t)w)));
 }
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ double lane_value(double v, int lane) {
+    const uint64_t w = (uint64_t)__double_as_longlong(v);
+    return __longlong_as_double((long long)((uint64_t)lane_value((uint32_t)(w >> 32), lane) << 32 | lane_value((uint32_t)w, lane)));
+}
+template <bool WAVE, bool SUM, typename T>
+__device__ __forceinline__ T reduced(T v) {
+#define ROWS_STEP(CTRL) { const T o = moved<CTRL>(v); if constexpr (SUM) v += o; else v = max(v, o); }
+    ROWS_STEP(0x111) ROWS_STEP(0x112) ROWS_STEP(0x114) ROWS_STEP(0x118)               // row_shr 1, 2, 4, 8
+    if constexpr (WAVE) { ROWS_STEP(0x142) ROWS_STEP(0x143) }                         // row_bcast 15, 31
+#undef ROWS_STEP
+    return lane_value(v, WAVE ? 63 : 15);
 }
 
 // fp32 + ROUNDER rounds to the nearest integer, ties to even, and has it (two's complement) in its low byte
@@ -183,7 +198,12 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
 #pragma unroll
         for (int v = 0; v < NV; v++) fetch(v, column(turn, v));
         if constexpr (KIND == ROWS_NORM) {
-            float d[NV][8];                                  // (all of a thread's reads are asked for before any is used)
+            float d[NV][8], g[NV][8];                        // (all of a thread's reads are asked for before any is used)
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                const int at = column(0, v), n = min(max(k - at, 0), 8);
+                if (n > 0) load8<true>(a.gain, at, n, g[v]);
+            }
             if (a.delta) {
 #pragma unroll
                 for (int v = 0; v < NV; v++) {
@@ -195,8 +215,6 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
             for (int v = 0; v < NV; v++) {
                 const int at = column(0, v), n = min(max(k - at, 0), 8);
                 if (n <= 0) continue;
-                float g[8];
-                load8<true>(a.gain, at, n, g);
                 if (a.delta) {
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
@@ -209,7 +227,7 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
                 for (int e = 0; e < 8; e++) {
                     const double hd = h[v][e];
                     sum = fma(hd, hd, sum);
-                    h[v][e] *= g[e];
+                    h[v][e] *= g[v][e];
                 }
             }
         }
@@ -220,8 +238,8 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
     }
     // the row's maximum (and sum of squares)
     const uint32_t mine_bits = top_bits;
-    top_bits = wave_max(top_bits);
-    if constexpr (KIND == ROWS_NORM) sum = wave_sum(sum);
+    top_bits = reduced<true, false>(top_bits);
+    if constexpr (KIND == ROWS_NORM) sum = reduced<true, true>(sum);
     if (lane == 0) {
         s_max[wave] = top_bits;
         if constexpr (KIND == ROWS_NORM) s_sum[wave] = sum;
@@ -230,13 +248,8 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
     __syncthreads();
     {
         const bool some = (lane & 15) < waves;               // 16 lanes take a wave's result each
-        top_bits = some ? s_max[lane & 15] : 0;
-        if constexpr (KIND == ROWS_NORM) sum = some ? s_sum[lane & 15] : 0.0;
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-            top_bits = max(top_bits, (uint32_t)__shfl_xor((int)top_bits, o, 64));
-            if constexpr (KIND == ROWS_NORM) sum += __shfl_xor(sum, o, 64);
-        }
+        top_bits = reduced<false, false>(some ? s_max[lane & 15] : 0u);
+        if constexpr (KIND == ROWS_NORM) sum = reduced<false, true>(some ? s_sum[lane & 15] : 0.0);
     }
     bool bad = top_bits >= 0x7F800000u;
     const float top32 = __uint_as_float(top_bits);
@@ -335,8 +348,8 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
 template <int KIND, bool XB, bool DB>
 static void launch_rows(const RowsArgs &a, int m, hipStream_t s) {
     // Few rows: as many waves as there are groups, for a row is latency.  Many: four waves and several rows a CU, up to four groups a
-    // thread for plain rows and two for the others, which compute more (four / two: 28672 rows of 8192 134 / 150 us; norm of 8192 rows of
-    // 8192 fp32 195 / 178, 4096 gated rows of 28672 172 / 165; one: 11008 rows of 4096 30 -> 36, norm of 8192 rows of 5120 78 -> 96).
+    // thread for plain rows and two for the others, which compute more (four / two: 28672 plain rows of 8192 bf16 131 / 137 us; norm of
+    // 8192 rows of 5120 bf16 96 / 78, of 8192 fp32 186 / 178; 4096 gated rows of 28672 bf16 170 / 162).
     constexpr int HELD = KIND == ROWS_PLAIN ? 4 : 2;
     const int groups = (a.k + 7) / 8, most = m >= ROWS_MANY ? 256 : 1024, needed = (groups + HELD - 1) / HELD;
     const int threads = max(min(most, (groups + 63) / 64 * 64), min(1024, (needed + 63) / 64 * 64)), nv = (groups + threads - 1) / threads;
