@@ -5,7 +5,7 @@
 //
 // Which side of a rounding border a value falls on is decided exactly for the norm and for plain rows, and in double for the
 // gating: two programs that agree on the inputs agree on every q.  A code is found in fp32 (relative error of 127 |v| / a below
-// 1e-6) and, where that lands within ROUND_MARGIN of a border, again in double.  The norm's row factor r > 0 scales v and a alike
+// 1e-6) and, where that lands too near to a border, again in double.  The norm's row factor r > 0 scales v and a alike
 // and drops out of q, so that v stands for h_i g_i, which a double holds exactly (24 + 8 bits); whether |v| is above, on or below
 // the border (k + 1/2) a / 127 is whether 254 |v| - (2k + 1) a is positive, zero or negative, both terms exact in a double.
 //
@@ -19,10 +19,11 @@
 
 enum { ROWS_PLAIN = 0, ROWS_NORM = 1, ROWS_GATE = 2 };
 
-// fp32 quotients 127 |v| / a are found again in double where they are this near to a border: 127 times their relative error, at
-// most 5 units of 2^-24 for the norm and plain rows and 9 for the gating (exponential 2, sum 1/2, reciprocal 1, four roundings of
-// products and of 127 / a, and that division's) = 7e-5.
-#define ROUND_MARGIN 1.0e-4f
+// fp32 quotients 127 |v| / a are found again in double where they are this near to a border: 127 times their relative error, in units
+// of 2^-24: 127 / a at most 2 and its product with v 1, for plain rows no more (2.3e-5); the norm's v and a, products, 1 each (3.8e-5); the
+// gating's v and a 8 each (exponential 2 and its correction 1, sum 1, reciprocal 2, two products; 1.44e-4).
+template <int KIND>
+constexpr float round_margin() { return KIND == 0 ? 2.5e-5f : KIND == 1 ? 4.0e-5f : 1.5e-4f; }
 // largest |v| of a row for which fp32 quotients have that error: 127 / a and all that matters are normal numbers
 #define PLAIN_RANGE_LO 1e-30f
 #define PLAIN_RANGE_HI 1e30f
@@ -254,24 +255,23 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
     bool bad = top_bits >= 0x7F800000u;
     const float top32 = __uint_as_float(top_bits);
     const bool in_range = top32 >= PLAIN_RANGE_LO && top32 <= PLAIN_RANGE_HI;
-    double top = top32;
     if constexpr (KIND != ROWS_PLAIN) {
         // the largest value in double: of those that fp32 has within its error of its largest (all, where fp32 does not hold them)
         const float near = in_range ? top32 * (1.0f - 1e-5f) : 0.f;
         if (!in_range || __uint_as_float(mine_bits) >= near) {
             unsigned long long best = 0;
             for (int turn = 0; turn < turns; turn++) {
-                uint64_t todo = 0;
+                uint32_t todo = 0;
 #pragma unroll
                 for (int v = 0; v < NV; v++) {
                     const int at = column(turn, v);
                     if constexpr (!KEEP) fetch(v, at);
 #pragma unroll
                     for (int e = 0; e < 8; e++)
-                        if (at + e < k && (!in_range || fabsf(h[v][e]) >= near)) todo |= 1ull << (8 * v + e);
+                        if (at + e < k && (!in_range || fabsf(h[v][e]) >= near)) todo |= 1u << (8 * v + e);
                 }
                 while (todo) {
-                    const int i = __builtin_ctzll(todo);
+                    const int i = __builtin_ctz(todo);
                     todo &= todo - 1;
                     const unsigned long long w = (unsigned long long)__double_as_longlong(exactly(column(turn, i >> 3) + (i & 7)));
                     best = max(best, w == NO_NUMBER ? w : w & ~(1ull << 63));
@@ -279,25 +279,21 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
             }
             if (best) atomicMax(&s_exact, best);
         }
-        __syncthreads();
-        top = __longlong_as_double((long long)s_exact);
-        if constexpr (KIND == ROWS_NORM) bad = s_exact == NO_NUMBER;
     }
-    if (tid == 0) {
-        double s = top / 127.0;
-        if constexpr (KIND == ROWS_NORM) s /= sqrt(sum / (double)k + a.eps);
-        a.scale[row] = bad ? __builtin_nanf("") : top == 0.0 ? 0.f : (float)s;
-    }
-    const bool none = bad || top == 0.0;
+    // the codes that fp32 decides are stored, the others' bits are returned: all of a row that fp32 does not hold
     const float c32 = 127.0f / top32;
-    for (int turn = 0; turn < turns; turn++) {
-        uint64_t todo = 0;                                   // values whose integer is found in double
+    auto round = [&](int turn) __attribute__((always_inline)) {
+        uint32_t todo = 0;
 #pragma unroll
         for (int v = 0; v < NV; v++) {
             const int at = column(turn, v);
             if constexpr (!KEEP) fetch(v, at);
             const int n = min(max(k - at, 0), 8);
             if (n <= 0) continue;
+            if (!in_range) {
+                todo |= (uint32_t)((1 << n) - 1) << (8 * v);
+                continue;
+            }
             float r[8], off = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
@@ -305,11 +301,10 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
                 r[e] = t + ROUNDER;
                 off = fmaxf(off, fabsf(t - (r[e] - ROUNDER)));
             }
-            if (!in_range) todo |= (uint64_t)((1 << n) - 1) << (8 * v);
-            else if (off > 0.5f - ROUND_MARGIN) {
+            if (off > 0.5f - round_margin<KIND>()) {
 #pragma unroll
                 for (int e = 0; e < 8; e++)
-                    if (e < n && fabsf(h[v][e] * c32 - (r[e] - ROUNDER)) > 0.5f - ROUND_MARGIN) todo |= 1ull << (8 * v + e);
+                    if (e < n && fabsf(h[v][e] * c32 - (r[e] - ROUNDER)) > 0.5f - round_margin<KIND>()) todo |= 1u << (8 * v + e);
             }
             uint32_t b[8];
 #pragma unroll
@@ -319,17 +314,47 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
 #pragma unroll
                 for (int e = 0; e < 2; e++) {
                     const uint32_t lo = __builtin_amdgcn_perm(b[4 * e + 1], b[4 * e], 0x0c0c0400), hi = __builtin_amdgcn_perm(b[4 * e + 3], b[4 * e + 2], 0x0c0c0400);
-                    w.w[e] = none ? 0u : lo | hi << 16;
+                    w.w[e] = lo | hi << 16;
                 }
                 *reinterpret_cast<Bytes8 *>(q + at) = w;
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; e++)
-                    if (e < n) q[at + e] = none ? 0 : (int8_t)(b[e] & 255);
+                    if (e < n) q[at + e] = (int8_t)(b[e] & 255);
             }
         }
-        while (todo && !none) {
-            const int i = __builtin_ctzll(todo), at = column(turn, i >> 3) + (i & 7);
+        return todo;
+    };
+    uint32_t todo = 0;
+    // (before the second barrier, while the few threads that refine the maximum wait for its sources: with narrower margins norm of 4096
+    // rows of 16384 bf16 64.6 -> 59.7 us, 11008 plain rows of 4096 27.9 -> 27.1, gating within 1 %)
+    if constexpr (KEEP) todo = round(0);
+    double top = top32;
+    if constexpr (KIND != ROWS_PLAIN) {
+        __syncthreads();
+        top = __longlong_as_double((long long)s_exact);
+        if constexpr (KIND == ROWS_NORM) bad = s_exact == NO_NUMBER;
+    }
+    const bool none = bad || top == 0.0;                     // (not in_range)
+    if (tid == 0) {
+        double s = top / 127.0;
+        if constexpr (KIND == ROWS_NORM) s /= sqrt(sum / (double)k + a.eps);
+        a.scale[row] = bad ? __builtin_nanf("") : top == 0.0 ? 0.f : (float)s;
+    }
+    for (int turn = 0; turn < turns; turn++) {
+        if constexpr (!KEEP) todo = round(turn);
+        if (none) {
+#pragma unroll
+            for (int v = 0; v < NV; v++) {
+                const int at = column(turn, v), n = min(max(k - at, 0), 8);
+                if (n == 8) *reinterpret_cast<Bytes8 *>(q + at) = Bytes8{};
+                else
+                    for (int e = 0; e < n; e++) q[at + e] = 0;
+            }
+            continue;
+        }
+        while (todo) {
+            const int i = __builtin_ctz(todo), at = column(turn, i >> 3) + (i & 7);
             todo &= todo - 1;
             const double p = exactly(at), m = fabs(p);
             double up;
