@@ -59,6 +59,7 @@ extern "C" {
 #define BITA_MAX_ROWS   512      /* R limit of one template                                   */
 #define BITA_MAX_TOPK    64      /* kmax limit                                                */
 #define BITA_Q8_MAX_LD (1 << 23) /* largest row stride of bita_gemm_q8's activations, bytes             */
+#define BITA_Q8_MAX_N (1 << 26)  /* most rows of an 8-bit weight                                       */
 #define BITA_Q8_MAX_K 131071     /* longest row of 8-bit integers: sums of 128 * 128 * K stay within 32 bits */
 
 /* Decoder shape.  LLaMA-2 architecture (the paper's base models, Sec. 4.1.2):
@@ -329,17 +330,19 @@ int bita_gemm_noalloc(const void *d_a, const void *d_a_lo, int32_t m_rows, int64
  * that v_i is q_i s within half a step; a row of zeros has q = 0, s = 0, and a row with a NaN or an infinity q = 0,
  * s = NaN (whatever it is multiplied with is NaN).  Every q is the exactly rounded one (bita_silu_mul_q8: rounded from double).
  * x_type, delta_type, out_type: BITA_F32 or BITA_BF16.  ld*: elements from one row to the next; any alignment and any
- * k is accepted, and rows whose start and stride are multiples of 16 bytes are the fast ones.  The outputs of the three
- * row calls do not overlap their inputs, except where stated.
+ * k is accepted (pointers are multiples of their element's size), and rows whose start and stride are multiples of 16 bytes are the fast
+ * ones.  No output of these calls overlaps an input or another output, except where stated.  Every call's buffers are on the current device.
  *
  * bita_quantize_rows  rows as they are: an attention output in front of its projection; a weight [N][K], one scale a channel.
  *                     1 <= k <= BITA_Q8_MAX_K
  * bita_norm_q8        h = x + delta (delta optional; added in fp32, rounded to x's type, stored in d_total, which may be
- *                     d_x with its stride), v = h / sqrt(mean(h^2) + eps) * gain, d_gain bf16 [d].  1 <= d <= 16384
+ *                     d_x with its stride; eps finite and at least 0), v = h / sqrt(mean(h^2) + eps) * gain, d_gain bf16 [d].  1 <= d <= 16384
  * bita_silu_mul_q8    v = silu(gate) * up of a gate/up product [M][2 d_ffn]: tile 16 = tiles of 16 gate columns, each followed
  *                     by its 16 up columns (bita_pack_weight's interleaving; d_ffn a multiple of 16), tile 0 = all gate columns
  *                     first.  1 <= d_ffn <= BITA_Q8_MAX_K
- * All three only enqueue one kernel on `stream`. */
+ *                     A product beyond fp32 counts as an infinity.
+ * A scale is rounded to fp32 (one beyond it, which only bita_norm_q8's gain can bring about, is an infinity).  All three only enqueue one kernel
+ * on `stream` (one for every 2^21 rows) and may be captured. */
 int bita_quantize_rows(const void *d_x, int32_t x_type, int32_t m_rows, int64_t k, int64_t ldx, int8_t *d_q, int64_t ldq,
                        float *d_scale, void *stream);
 int bita_norm_q8(const void *d_x, int32_t x_type, int32_t m_rows, int64_t d, int64_t ldx, const void *d_delta, int32_t delta_type,
@@ -351,18 +354,19 @@ int bita_silu_mul_q8(const void *d_gate_up, int32_t x_type, int32_t m_rows, int6
 /* The packed form of an 8-bit weight [N][K]: 1 KiB blocks, each one MFMA operand (16 rows x 64 k), ordered
  * [pair of k-steps][16-row tile][k-step of the pair]; K is padded with zeros to a multiple of 128, N to one of 16.
  * Arguments as bita_pack_weight's, but for d_src: signed 8-bit integers, `ld` apart (any k and alignment; n_rows a multiple of
- * 16 unless the source's last tile is the destination's last).  d_dst holds bita_packed_q8_bytes(dst_total_rows, k). */
+ * 16 unless the source's last tile is the destination's last; at most BITA_Q8_MAX_N).  d_dst holds bita_packed_q8_bytes(dst_total_rows, k). */
 size_t bita_packed_q8_bytes(int64_t n_rows, int64_t k);
 int bita_pack_weight_q8(const int8_t *d_src, int64_t n_rows, int64_t k, int64_t ld, void *d_dst, int64_t dst_total_rows,
                         int64_t dst_tile0, int64_t dst_tile_stride, void *stream);
 
-/* d_out[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n]: the sums are 32-bit integers and exact, each multiplied
- * in fp32 by the row's scale, then by the channel's, and rounded once more where out_type is BITA_BF16.
+/* d_out[m][n] = (sum_k a[m][k] w[n][k]) * a_scale[m] * w_scale[n]: the sums are 32-bit integers and exact, each rounded to fp32, multiplied
+ * there by the row's scale, then by the channel's, and rounded once more where out_type is BITA_BF16.
  *   d_a [m_rows][lda] 8-bit integers, as the row calls leave them: d_a and lda multiples of 16, k <= lda <= BITA_Q8_MAX_LD.  Columns
  *   from k to the next multiple of 16 may hold anything, and are read (of the last row too).  d_w_scale is in the order of the packed
- *   rows.  1 <= k <= BITA_Q8_MAX_K; any m_rows, n_rows, ldo >= n_rows and alignment of d_out.
+ *   rows.  1 <= k <= BITA_Q8_MAX_K, 1 <= n_rows <= BITA_Q8_MAX_N; any m_rows, ldo >= n_rows and alignment of d_out.
  * d_ws: bita_gemm_q8_workspace_bytes() bytes of scratch at a multiple of 16 (the sums of a launch whose k is split; 0 bytes where it is not, and
- * d_ws may then be NULL); nothing in it is kept from call to call.  One kernel, or two where k is split.
+ * d_ws may then be NULL; fewer rows can need more than more rows do); nothing in it is kept from call to call, and calls that may run at
+ * the same time have each their own.  One kernel, or two where k is split; may be captured.
  * bita_gemm_q8_plan_info: how a product of these sizes is cut (for tests and reports): out4 (HOST) = {rows and columns of a workgroup, k splits,
  * 1 for the kernel of few rows, 0 for tiles of many}. */
 size_t bita_gemm_q8_workspace_bytes(int32_t m_rows, int64_t n_rows, int64_t k);

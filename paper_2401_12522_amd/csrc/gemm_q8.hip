@@ -513,12 +513,12 @@ extern "C" int bita_pack_weight_q8(const int8_t *d_src, int64_t n_rows, int64_t 
                                    int64_t dst_tile0, int64_t dst_tile_stride, void *stream) {
     if (!d_src || !d_dst || n_rows <= 0 || k <= 0 || ld < k || dst_tile0 < 0 || dst_tile_stride < 1 || (uintptr_t)d_dst % 16)
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_pack_weight_q8: bad argument");
-    const int64_t tiles = (n_rows + 15) / 16, total = (dst_total_rows + 15) / 16, last = dst_tile0 + (tiles - 1) * dst_tile_stride;
-    if (last >= total)
+    const int64_t tiles = (n_rows + 15) / 16, total = (dst_total_rows + 15) / 16, last = (int64_t)((uint64_t)dst_tile0 + (uint64_t)(tiles - 1) * (uint64_t)dst_tile_stride);
+    if (dst_tile0 >= total || (tiles > 1 && dst_tile_stride >= total) || last >= total)      // (the first two: `last` did not wrap)
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_pack_weight_q8: source tiles do not fit %lld destination rows", (long long)dst_total_rows);
     if (n_rows % 16 && last != total - 1)
         return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_pack_weight_q8: %lld rows end inside a tile that is not the destination's last", (long long)n_rows);
-    if (k > BITA_Q8_MAX_K || tiles > INT32_MAX)
+    if (k > BITA_Q8_MAX_K || n_rows > BITA_Q8_MAX_N)
         return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_pack_weight_q8: %lld rows of %lld", (long long)n_rows, (long long)k);
     hipLaunchKernelGGL(pack_q8_kernel, dim3((unsigned)tiles, (unsigned)min((int64_t)8, (k + 255) / 256)), dim3(256), 0, (hipStream_t)stream, d_src, n_rows,
                        k, ld, (uint4 *)d_dst, dst_tile0, dst_tile_stride, total);
@@ -529,12 +529,12 @@ extern "C" int bita_pack_weight_q8(const int8_t *d_src, int64_t n_rows, int64_t 
 static size_t plan_bytes(const PlanQ8 &p, int m, int64_t n) { return p.splits > 1 ? (size_t)p.splits * m * (size_t)((n + 15) / 16 * 16) * 4 : 0; }
 
 extern "C" size_t bita_gemm_q8_workspace_bytes(int32_t m_rows, int64_t n_rows, int64_t k) {
-    if (m_rows <= 0 || n_rows <= 0 || k <= 0 || k > BITA_Q8_MAX_K) return 0;
+    if (m_rows <= 0 || n_rows <= 0 || k <= 0 || k > BITA_Q8_MAX_K || n_rows > BITA_Q8_MAX_N) return 0;
     return plan_bytes(plan_q8(m_rows, n_rows, (int)((k + 127) / 128)), m_rows, n_rows);
 }
 
 extern "C" int bita_gemm_q8_plan_info(int32_t m_rows, int64_t n_rows, int64_t k, int32_t *out4) {
-    if (!out4 || m_rows <= 0 || n_rows <= 0 || k <= 0 || k > BITA_Q8_MAX_K)
+    if (!out4 || m_rows <= 0 || n_rows <= 0 || k <= 0 || k > BITA_Q8_MAX_K || n_rows > BITA_Q8_MAX_N)
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_gemm_q8_plan_info: bad argument");
     const PlanQ8 p = plan_q8(m_rows, n_rows, (int)((k + 127) / 128));
     const bool skinny = p.form >= SKINNY;
@@ -552,8 +552,9 @@ extern "C" int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_sca
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_gemm_q8: bad argument");
     if ((uintptr_t)d_a % 16 || (uintptr_t)d_w_packed % 16 || lda % 16 || (m_rows > 1 && lda < k) || (uintptr_t)d_out % (out_type == BITA_BF16 ? 2 : 4))
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_gemm_q8: d_a, d_w_packed and lda have to be multiples of 16, lda at least k");
-    if (k > BITA_Q8_MAX_K || lda > BITA_Q8_MAX_LD)
-        return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_gemm_q8: k %lld, lda %lld, at most %d and %d", (long long)k, (long long)lda, BITA_Q8_MAX_K, BITA_Q8_MAX_LD);
+    if (k > BITA_Q8_MAX_K || lda > BITA_Q8_MAX_LD || n_rows > BITA_Q8_MAX_N)
+        return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_gemm_q8: k %lld, lda %lld, n_rows %lld, at most %d, %d and %d", (long long)k, (long long)lda,
+                              (long long)n_rows, BITA_Q8_MAX_K, BITA_Q8_MAX_LD, BITA_Q8_MAX_N);
     const int k_pairs = (int)((k + 127) / 128), k16 = (int)((k + 15) / 16 * 16);
     const PlanQ8 p = plan_q8(m_rows, n_rows, k_pairs);
     const size_t need = plan_bytes(p, m_rows, n_rows);

@@ -370,22 +370,32 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------
+#define ROWS_A_LAUNCH (1 << 21)        // (a grid has less than 2^32 threads)
 template <int KIND, bool XB, bool DB>
-static void launch_rows(const RowsArgs &a, int m, hipStream_t s) {
+static void launch_rows(RowsArgs a, int m, hipStream_t s) {
     // Few rows: as many waves as there are groups, for a row is latency.  Many: four waves and several rows a CU, up to four groups a
     // thread for plain rows and two for the others, which compute more (four / two: 28672 plain rows of 8192 bf16 131 / 137 us; norm of
     // 8192 rows of 5120 bf16 96 / 78, of 8192 fp32 186 / 178; 4096 gated rows of 28672 bf16 170 / 162).
     constexpr int HELD = KIND == ROWS_PLAIN ? 4 : 2;
     const int groups = (a.k + 7) / 8, most = m >= ROWS_MANY ? 256 : 1024, needed = (groups + HELD - 1) / HELD;
     const int threads = max(min(most, (groups + 63) / 64 * 64), min(1024, (needed + 63) / 64 * 64)), nv = (groups + threads - 1) / threads;
-#define ROWS_LAUNCH(NV, KEEP) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, NV, KEEP>), dim3(m), dim3(threads), 0, s, a)
-    if (nv <= 1) ROWS_LAUNCH(1, true);
-    else if (KIND == ROWS_NORM || nv <= 2) ROWS_LAUNCH(2, true);      // (1024 threads of two groups: the norm's longest row)
-    else if constexpr (KIND != ROWS_NORM) {
-        if (nv <= 4) ROWS_LAUNCH(4, true);
-        else ROWS_LAUNCH(2, false);
-    }
+    for (int left = m; left > 0; left -= ROWS_A_LAUNCH) {
+        const dim3 grid(min(left, ROWS_A_LAUNCH));
+#define ROWS_LAUNCH(NV, KEEP) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, NV, KEEP>), grid, dim3(threads), 0, s, a)
+        if (nv <= 1) ROWS_LAUNCH(1, true);
+        else if (KIND == ROWS_NORM || nv <= 2) ROWS_LAUNCH(2, true);      // (1024 threads of two groups: the norm's longest row)
+        else if constexpr (KIND != ROWS_NORM) {
+            if (nv <= 4) ROWS_LAUNCH(4, true);
+            else ROWS_LAUNCH(2, false);
+        }
 #undef ROWS_LAUNCH
+        const int64_t done = ROWS_A_LAUNCH;
+        a.x = (const char *)a.x + done * a.ldx * (XB ? 2 : 4);
+        if (a.delta) a.delta = (const char *)a.delta + done * a.ld_delta * (DB ? 2 : 4);
+        if (a.delta) a.total = (char *)a.total + done * a.ld_total * (XB ? 2 : 4);
+        a.q += done * a.ldq;
+        a.scale += done;
+    }
 }
 
 static bool type_ok(int32_t t) { return t == BITA_F32 || t == BITA_BF16; }
@@ -424,7 +434,7 @@ extern "C" int bita_norm_q8(const void *d_x, int32_t x_type, int32_t m_rows, int
                             int32_t delta_type, int64_t ld_delta, const void *d_gain, float eps, void *d_total, int64_t ld_total,
                             int8_t *d_q, int64_t ldq, float *d_scale, void *stream) {
     if (!d_x || !d_gain || !d_q || !d_scale || m_rows <= 0 || d <= 0 || !type_ok(x_type) || !at_element(d_x, x_type) ||
-        !at_element(d_gain, BITA_BF16) || ldx < d || ldq < d || !(eps >= 0.f) ||
+        !at_element(d_gain, BITA_BF16) || ldx < d || ldq < d || !(eps >= 0.f && eps <= 3.4e38f) ||
         (d_delta && (!type_ok(delta_type) || !at_element(d_delta, delta_type) || !at_element(d_total, x_type) || ld_delta < d || !d_total || ld_total < d)))
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_norm_q8: bad argument");
     if (d > 1024 * RMS_MAX_CHUNKS)

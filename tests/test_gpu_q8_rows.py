@@ -187,6 +187,27 @@ def test_strides_offsets_and_what_lies_around_the_rows():
             assert bool((qbig == 99).all()) and float(sbig[0]) == float(sbig[-1]) == -1
 
 
+@pytest.mark.parametrize("call", ["rows", "norm", "gate"])
+def test_more_rows_than_a_launch_has(call):
+    import paper_2401_12522_amd as bita
+    m, k = (1 << 21) + 5, 9
+    x = rows(m, 2 * k if call == "gate" else k, 5, torch.bfloat16)
+    if call == "rows":
+        q, s = bita.quantize_rows(x)
+        v, factor = x.double(), None
+    elif call == "norm":
+        delta, total, gain = rows(m, k, 6, torch.float32), torch.empty_like(x), rows(1, k, 7, torch.bfloat16, 0.1)[0]
+        q, s = bita.norm_q8(x, gain, 1e-5, delta=delta, total=total)
+        h = (x.float() + delta).bfloat16()
+        assert torch.equal(total, h)
+        v, factor = h.double() * gain.double(), 1 / torch.sqrt(h.double().square().mean(1) + 1e-5)
+    else:
+        q, s = bita.silu_mul_q8(x)
+        g, u = x[:, :k].double(), x[:, k:].double()
+        v, factor = g / (1 + torch.exp(-g)) * u, None
+    check(q, s, v, factor)
+
+
 def test_refusals_of_the_binding():
     import paper_2401_12522_amd as bita
     x = rows(4, 64, 1, torch.float32)

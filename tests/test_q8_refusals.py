@@ -50,6 +50,22 @@ def test_refused_with_a_message(name, good, bad, code):
     assert name.encode() in _lib().bita_last_error()
 
 
+@pytest.mark.parametrize("name,good,bad,code", [
+    # strides whose last tile's number wraps around 64 bits
+    ("bita_pack_weight_q8", PACK, dict(stride=(1 << 63) - 1), -1), ("bita_pack_weight_q8", dict(PACK, n=80), dict(stride=1 << 62), -1),
+    ("bita_pack_weight_q8", PACK, dict(tile0=(1 << 63) - 1), -1),
+    ("bita_pack_weight_q8", PACK, dict(n=(1 << 26) + 16, total=1 << 27), -4), ("bita_gemm_q8", GEMM, dict(n=(1 << 26) + 1, ldo=1 << 27), -4),
+    ("bita_norm_q8", NORM, dict(eps=float("inf")), -1),
+])
+def test_refused_beyond_a_launch(name, good, bad, code):
+    test_refused_with_a_message(name, good, bad, code)
+
+
+def test_workspace_of_refused_sizes():
+    L = _lib()
+    assert L.bita_gemm_q8_workspace_bytes(4, (1 << 26) + 1, 4096) == L.bita_gemm_q8_workspace_bytes(4, 64, 131072) == 0
+
+
 def test_packed_sizes():
     L = _lib()
     assert L.bita_packed_q8_bytes(32, 688) == 2 * 6 * 2048
