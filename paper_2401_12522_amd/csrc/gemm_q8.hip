@@ -342,7 +342,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
     // 32 rows a store; so a wave turns 32 rows at a time in LDS of its own (16 bytes more a row: rows start in different banks).  Straight from the
     // registers 4096 rows of 22016 x 4096 in bf16 took 100 us longer than without stores.
     constexpr int COLS = 32 * NF, LD = COLS / 4 + 1;                                  // in 16-byte pieces
-    static_assert(WAVES * 32 * LD <= 2 * STAGE, "the epilogue's rows fit the stages");
+    static_assert(WAVES * 32 * LD <= 2 * STAGE && (NF & (NF - 1)) == 0, "the epilogue's rows fit the stages, its lanes divide a wave");
     i32x4 *own = lds + wave * 32 * LD;
     auto leave = [&](auto *o, int64_t ldo, int64_t n) __attribute__((always_inline)) {
         constexpr int V = 16 / (int)sizeof(*o), LANES = COLS / V, ROWS = 64 / LANES;  // columns of a lane, lanes of a row, rows a store
@@ -388,26 +388,30 @@ struct GemmQ8 {
 enum { SKINNY = 16 };
 struct PlanQ8 { int form, mt, splits, split_steps; };
 
-// Tile kernels: rows and columns of a workgroup, and the time of 128 k of one, us (1024 rows x 4096 x 4096 in one round)
+// Tile kernels: rows and columns of a workgroup, and the time of 128 k of one, us (1024 rows x 4096 x 4096 in one round, 288 x 128 at 272 rows of
+// 22016 x 4096: 49 us, with 160 x 256 57, 96 x 192 53).  The times follow the bytes of a stage, 32 to 42 GB/s a CU: half as many waves of
+// twice the columns, with fewer LDS reads, are no faster (160 x 256 by four waves 58).
 struct TileForm { int rows, cols; float stage; };
-static const TileForm TILE_FORMS[] = {{256, 256, 2.06f}, {160, 256, 1.53f}, {128, 256, 1.16f}, {128, 128, 0.82f}, {96, 192, 0.90f}};
+static const TileForm TILE_FORMS[] = {{256, 256, 2.06f}, {160, 256, 1.53f}, {128, 256, 1.16f}, {128, 128, 0.82f}, {96, 192, 0.90f}, {288, 128, 1.36f}};
 static const int SKINNY_WIDE[] = {1, 2, 3, 4, 6, 8};
 #define SKINNY_MAX_MT 9
 
 // Whichever form promises the least time.  What the estimates rest on (measured):
-//  * a CU has about 32 KB of vector loads in flight and gets them in order: 52 GB/s of weights and activations together where the
+//  * a CU has about 32 KB of vector loads in flight and gets them in order: 56 GB/s of weights and activations together where the
 //    weights come from HBM, whatever is behind its L1; hence few rows are cut so that all 256 CUs work and a workgroup's rows,
 //    which every workgroup reads, are amortised over many columns, by splitting k if need be;
-//  * weights alone arrive at 6.3 TB/s; a launch costs 3.5 us and 1.5 more for each further round of workgroups, a second one (the splits' sums) 3 us and its traffic;
-//  * above five row tiles the skinny kernel's LDS reads, one per matrix instruction, no longer hide behind the loads (x 1.5).
+//  * the few-rows kernel reads LDS once for each matrix instruction: 0.012 us a stage for each of its tiles of 16 x 16;
+//  * weights alone arrive at 6.3 TB/s; a launch costs 3.5 us and 1.5 more for each further round of workgroups, a second one (the splits' sums) 3 us and its traffic.
+// With every form and split of 148 products of 1 to 1024 rows timed, its choices are 1.0 % slower than the best in the mean and 15 % at most.
 static PlanQ8 plan_q8(int m, int64_t n, int k_pairs) {
     const int64_t n_tiles = (n + 15) / 16;
     const int stages = (k_pairs + 3) / 4;
-    PlanQ8 best = {0, 0, 1, 2 * k_pairs};
+    PlanQ8 best = {};
     double best_us = 1e30;
     const double weights_us = 2048.0 * n_tiles * k_pairs / 6.3e6;
     const auto sums_us = [&](int splits) { return splits > 1 ? 3 + 8.0 * splits * m * (16.0 * n_tiles) / 4.5e6 : 0.0; };
-    for (int f = 0; f < (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])); f++)
+    const int forms = m > 16 ? (int)(sizeof(TILE_FORMS) / sizeof(TILE_FORMS[0])) : 0;       // (16 rows of 57344 x 8192: 75 us, in tiles of 128 80)
+    for (int f = 0; f < forms; f++)
         for (int splits = 1; splits <= 8 && (splits == 1 || splits * 8 <= k_pairs); splits++) {
             const TileForm &t = TILE_FORMS[f];
             const int per = (k_pairs + splits - 1) / splits;
@@ -426,9 +430,8 @@ static PlanQ8 plan_q8(int m, int64_t n, int k_pairs) {
             if (s != splits) continue;
             const double groups = (double)((n_tiles + wide - 1) / wide) * blocks * splits, rounds = ceil(groups / 256);
             const double bytes = 512.0 * ((m + blocks - 1) / blocks + 16 * wide);
-            const double stage = fmax(0.34, bytes / 52e3 * (mt > 5 ? 1.5 : 1.0));
-            double us = 2 + 1.5 * rounds + fmax(rounds * per * stage, weights_us);
-            us += sums_us(splits);
+            const double stage = fmax(0.34, bytes / 56e3 + 0.012 * mt * wide);
+            const double us = 2 + 1.5 * rounds + fmax(rounds * per * stage, weights_us) + sums_us(splits);
             if (us < best_us) { best_us = us; best = {SKINNY + wide, mt, splits, 8 * per}; }
         }
     }
@@ -488,7 +491,8 @@ static void launch_gemm_q8(const GemmQ8 &g, const PlanQ8 &p) {
             case 1: return launch_tile<5, 1, 1, 8>(g, p);
             case 2: return launch_tile<2, 2, 2, 4>(g, p);
             case 3: return launch_tile<2, 1, 2, 4>(g, p);
-            default: return launch_tile<3, 1, 1, 6>(g, p);
+            case 4: return launch_tile<3, 1, 1, 6>(g, p);
+            default: return launch_tile<3, 2, 3, 2>(g, p);
         }
     }
     switch (p.mt) {

@@ -48,11 +48,12 @@ def test_product(m, n, k, dtype):
 
 @pytest.mark.parametrize("m,n,k,rows,cols,splits", [
     # every workgroup shape, k whole and split, ragged at every end
-    (3, 64, 28672, 16, 16, 8), (16, 200, 9000, 16, 16, 4), (1, 4165, 107515, 16, 32, 1), (39, 8303, 10455, 48, 48, 1), (34, 3166, 21811, 48, 64, 4), (50, 28702, 2, 64, 128, 1),
+    (3, 64, 28672, 16, 16, 8), (16, 200, 9000, 16, 16, 4), (1, 4165, 107515, 16, 32, 1), (39, 8303, 10455, 48, 128, 3), (34, 3166, 21811, 48, 64, 5), (50, 28702, 2, 64, 128, 1),
     (68, 1037, 11000, 80, 32, 5), (83, 3006, 23350, 96, 96, 8), (86, 916, 119981, 96, 32, 8), (109, 32758, 374, 112, 128, 1), (117, 1504, 61018, 128, 48, 8), (144, 22016, 300, 144, 128, 1),
-    (275, 4021, 189, 144, 32, 1), (160, 48, 131071, 80, 16, 8), (79, 79711, 905, 96, 192, 1), (144, 500, 9001, 128, 128, 8), (700, 300, 20000, 128, 128, 8),
+    (275, 4021, 189, 144, 32, 1), (160, 48, 131071, 80, 16, 8), (79, 79711, 905, 96, 192, 1), (144, 500, 9001, 144, 16, 4), (700, 300, 20000, 128, 128, 8),
     (300, 100, 131071, 128, 128, 8), (1500, 130, 4001, 128, 128, 4), (149, 34781, 21400, 160, 256, 3), (293, 32003, 400, 160, 256, 1), (520, 9000, 400, 128, 256, 1),
-    (898, 12646, 1507, 256, 256, 1)])
+    (898, 12646, 1507, 256, 256, 1), (33, 8313, 16, 48, 48, 1), (135, 5457, 7824, 144, 128, 4), (281, 22543, 16, 288, 128, 1), (281, 22543, 515, 288, 128, 1),
+    (4244, 283, 5726, 288, 128, 5)])
 def test_workgroup_shapes(m, n, k, rows, cols, splits):
     import paper_2401_12522_amd as bita
     plan = bita.binding.gemm_q8_plan_info(m, n, k)
