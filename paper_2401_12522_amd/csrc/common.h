@@ -254,6 +254,12 @@ __device__ __forceinline__ int tree_token(const BuildSource &s, const TemplateDe
     return (g >= 0 && lvl >= 0 && lvl < t.n_mask && row < s.cand_rows && rank < s.kmax)
                ? s.cand[((int64_t)b * s.cand_rows + row) * s.kmax + rank] : -1;
 }
+// 8-bit layers: sums of an 8-bit product whose k was split, [splits][m][n] (n a multiple of 16), and the scales that go with them; splits 0: none,
+// the product's own output holds it.  gemm_q8 leaves them to its consumer where `left` is given; norm_q8_of_sums adds them to x (in place) instead of a delta.
+struct SumsQ8 { const int *part; int splits; const float *row_scale, *col_scale; };
+int gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t m_rows, int64_t k, const void *d_w_packed, const float *d_w_scale, int64_t n_rows,
+            void *d_ws, size_t ws_bytes, void *d_out, int32_t out_type, int64_t ldo, SumsQ8 *left, hipStream_t s);
+int norm_q8_of_sums(float *d_x, int m_rows, int64_t d, const SumsQ8 &delta, const void *d_gain, float eps, int8_t *d_q, int64_t ldq, float *d_scale, hipStream_t s);
 // the same for a bf16 matrix in rows (8-bit layers): [batch * rows][k] and [batch * rows][d] -> [batch][k] and [batch][d]
 void launch_gather_plain_rows(const int32_t *sel_row, int batch, int rows, const void *a, int k, const float *x, int d, void *a_out,
                               float *x_out, hipStream_t s);

@@ -549,8 +549,8 @@ extern "C" int bita_gemm_q8_plan_info(int32_t m_rows, int64_t n_rows, int64_t k,
     return BITA_OK;
 }
 
-extern "C" int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t m_rows, int64_t k, const void *d_w_packed,
-                            const float *d_w_scale, int64_t n_rows, void *d_ws, size_t ws_bytes, void *d_out, int32_t out_type, int64_t ldo, void *stream) {
+int gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t m_rows, int64_t k, const void *d_w_packed, const float *d_w_scale, int64_t n_rows,
+            void *d_ws, size_t ws_bytes, void *d_out, int32_t out_type, int64_t ldo, SumsQ8 *left, hipStream_t s) {
     if (!d_a || !d_a_scale || !d_w_packed || !d_w_scale || !d_out || m_rows <= 0 || k <= 0 || n_rows <= 0 || ldo < n_rows ||
         (out_type != BITA_F32 && out_type != BITA_BF16))
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_gemm_q8: bad argument");
@@ -564,9 +564,15 @@ extern "C" int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_sca
     const size_t need = plan_bytes(p, m_rows, n_rows);
     if (need && (!d_ws || ws_bytes < need || (uintptr_t)d_ws % 16))
         return bita_set_error(BITA_ERR_CAPACITY, "bita_gemm_q8: workspace %zu < %zu bytes, or not a multiple of 16", d_ws ? ws_bytes : (size_t)0, need);
-    const GemmQ8 g = {d_a, lda, d_a_scale, m_rows, k_pairs, k16, (const i32x4 *)d_w_packed, d_w_scale, n_rows, d_out, out_type, ldo, (int *)d_ws, (hipStream_t)stream};
+    const GemmQ8 g = {d_a, lda, d_a_scale, m_rows, k_pairs, k16, (const i32x4 *)d_w_packed, d_w_scale, n_rows, d_out, out_type, ldo, (int *)d_ws, s};
     launch_gemm_q8(g, p);
-    if (p.splits > 1) launch_reduce(g, p);
+    if (left) *left = p.splits > 1 ? SumsQ8{g.part, p.splits, d_a_scale, d_w_scale} : SumsQ8{};
+    else if (p.splits > 1) launch_reduce(g, p);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
+}
+
+extern "C" int bita_gemm_q8(const int8_t *d_a, int64_t lda, const float *d_a_scale, int32_t m_rows, int64_t k, const void *d_w_packed,
+                            const float *d_w_scale, int64_t n_rows, void *d_ws, size_t ws_bytes, void *d_out, int32_t out_type, int64_t ldo, void *stream) {
+    return gemm_q8(d_a, lda, d_a_scale, m_rows, k, d_w_packed, d_w_scale, n_rows, d_ws, ws_bytes, d_out, out_type, ldo, nullptr, (hipStream_t)stream);
 }

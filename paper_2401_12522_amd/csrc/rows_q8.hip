@@ -39,6 +39,8 @@ struct RowsArgs {
     int8_t *q;
     float *scale;
     int64_t ldx, ld_delta, ld_total, ldq;
+    SumsQ8 sums;                      // ROWS_NORM, SUMS: the delta (`delta` is sums.part)
+    int64_t sums_step;                // from one split's to the next
     int k, tile;                      // ROWS_GATE: columns of a gate tile (its up tile follows), 16 or k
     double eps;
 };
@@ -134,9 +136,33 @@ __device__ __forceinline__ T reduced(T v) {
 // fp32 + ROUNDER rounds to the nearest integer, ties to even, and has it (two's complement) in its low byte
 #define ROUNDER 12582912.0f
 
+// The delta's type where it is the sums of a product
+#define SUMS 2
+// eight neighbouring ones, as the product itself would store them in fp32
+__device__ __forceinline__ void load8_of_sums(const RowsArgs &a, int row, int at, float row_scale, float v[8]) {
+    typedef __attribute__((ext_vector_type(4))) int i32x4;
+    const int *part = a.sums.part + (int64_t)row * a.k + at;
+    i32x4 sum[2] = {};
+    for (int s0 = 0; s0 < a.sums.splits; s0 += 4) {
+        i32x4 q[4][2];
+#pragma unroll
+        for (int s = 0; s < 4; s++)                          // (requested together; those past the last are left out)
+#pragma unroll
+            for (int e = 0; e < 2; e++) q[s][e] = reinterpret_cast<const i32x4 *>(part + min(s0 + s, a.sums.splits - 1) * a.sums_step)[e];
+#pragma unroll
+        for (int s = 0; s < 4; s++)
+#pragma unroll
+            for (int e = 0; e < 2; e++)
+                if (s0 + s < a.sums.splits) sum[e] += q[s][e];
+    }
+    const float *scale = a.sums.col_scale + at;
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = (float)sum[e >> 2][e & 3] * row_scale * scale[e];
+}
+
 // NV groups of 8 values per thread are held in registers.  KEEP false (rows longer than a workgroup holds; not the norm): the
 // groups go round and the row is read again, mostly from cache.
-template <int KIND, bool XB, bool DB, int NV, bool KEEP>
+template <int KIND, bool XB, int DT, int NV, bool KEEP>
 __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
     static_assert(KEEP || KIND != ROWS_NORM, "the norm holds its row");
     __shared__ uint32_t s_max[16];
@@ -206,10 +232,14 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
                 if (n > 0) load8<true>(a.gain, at, n, g[v]);
             }
             if (a.delta) {
+                float row_scale = 0.f;
+                if constexpr (DT == SUMS) row_scale = a.sums.row_scale[row];        // (may be `scale`, which is written behind the barriers)
 #pragma unroll
                 for (int v = 0; v < NV; v++) {
                     const int at = column(0, v), n = min(max(k - at, 0), 8);
-                    if (n > 0) load8<DB>((const char *)a.delta + (int64_t)row * a.ld_delta * (DB ? 2 : 4), at, n, d[v]);
+                    if (n <= 0) continue;
+                    if constexpr (DT == SUMS) load8_of_sums(a, row, at, row_scale, d[v]);
+                    else load8<DT == BITA_BF16>((const char *)a.delta + (int64_t)row * a.ld_delta * (DT == BITA_BF16 ? 2 : 4), at, n, d[v]);
                 }
             }
 #pragma unroll
@@ -371,7 +401,7 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
 
 // ---------------------------------------------------------------------------------------
 #define ROWS_A_LAUNCH (1 << 21)        // (a grid has less than 2^32 threads)
-template <int KIND, bool XB, bool DB>
+template <int KIND, bool XB, int DT>
 static void launch_rows(RowsArgs a, int m, hipStream_t s) {
     // Few rows: as many waves as there are groups, for a row is latency.  Many: four waves and several rows a CU, up to four groups a
     // thread for plain rows and two for the others, which compute more (four / two: 28672 plain rows of 8192 bf16 131 / 137 us; norm of
@@ -381,7 +411,7 @@ static void launch_rows(RowsArgs a, int m, hipStream_t s) {
     const int threads = max(min(most, (groups + 63) / 64 * 64), min(1024, (needed + 63) / 64 * 64)), nv = (groups + threads - 1) / threads;
     for (int left = m; left > 0; left -= ROWS_A_LAUNCH) {
         const dim3 grid(min(left, ROWS_A_LAUNCH));
-#define ROWS_LAUNCH(NV, KEEP) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DB, NV, KEEP>), grid, dim3(threads), 0, s, a)
+#define ROWS_LAUNCH(NV, KEEP) hipLaunchKernelGGL((rows_q8_kernel<KIND, XB, DT, NV, KEEP>), grid, dim3(threads), 0, s, a)
         if (nv <= 1) ROWS_LAUNCH(1, true);
         else if (KIND == ROWS_NORM || nv <= 2) ROWS_LAUNCH(2, true);      // (1024 threads of two groups: the norm's longest row)
         else if constexpr (KIND != ROWS_NORM) {
@@ -391,7 +421,8 @@ static void launch_rows(RowsArgs a, int m, hipStream_t s) {
 #undef ROWS_LAUNCH
         const int64_t done = ROWS_A_LAUNCH;
         a.x = (const char *)a.x + done * a.ldx * (XB ? 2 : 4);
-        if (a.delta) a.delta = (const char *)a.delta + done * a.ld_delta * (DB ? 2 : 4);
+        if (DT == SUMS) a.sums.part += done * a.k, a.sums.row_scale += done;
+        else if (a.delta) a.delta = (const char *)a.delta + done * a.ld_delta * (DT == BITA_BF16 ? 2 : 4);
         if (a.delta) a.total = (char *)a.total + done * a.ld_total * (XB ? 2 : 4);
         a.q += done * a.ldq;
         a.scale += done;
@@ -408,8 +439,8 @@ extern "C" int bita_quantize_rows(const void *d_x, int32_t x_type, int32_t m_row
     if (k > BITA_Q8_MAX_K) return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_quantize_rows: k %lld, at most %d", (long long)k, BITA_Q8_MAX_K);
     RowsArgs a = {};
     a.x = d_x; a.q = d_q; a.scale = d_scale; a.ldx = ldx; a.ldq = ldq; a.k = (int)k;
-    if (x_type == BITA_BF16) launch_rows<ROWS_PLAIN, true, false>(a, m_rows, (hipStream_t)stream);
-    else launch_rows<ROWS_PLAIN, false, false>(a, m_rows, (hipStream_t)stream);
+    if (x_type == BITA_BF16) launch_rows<ROWS_PLAIN, true, BITA_F32>(a, m_rows, (hipStream_t)stream);
+    else launch_rows<ROWS_PLAIN, false, BITA_F32>(a, m_rows, (hipStream_t)stream);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
 }
@@ -424,8 +455,8 @@ extern "C" int bita_silu_mul_q8(const void *d_gate_up, int32_t x_type, int32_t m
     if (d_ffn > BITA_Q8_MAX_K) return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_silu_mul_q8: d_ffn %lld, at most %d", (long long)d_ffn, BITA_Q8_MAX_K);
     RowsArgs a = {};
     a.x = d_gate_up; a.q = d_q; a.scale = d_scale; a.ldx = ldx; a.ldq = ldq; a.k = (int)d_ffn; a.tile = tile ? tile : (int)d_ffn;
-    if (x_type == BITA_BF16) launch_rows<ROWS_GATE, true, false>(a, m_rows, (hipStream_t)stream);
-    else launch_rows<ROWS_GATE, false, false>(a, m_rows, (hipStream_t)stream);
+    if (x_type == BITA_BF16) launch_rows<ROWS_GATE, true, BITA_F32>(a, m_rows, (hipStream_t)stream);
+    else launch_rows<ROWS_GATE, false, BITA_F32>(a, m_rows, (hipStream_t)stream);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
 }
@@ -447,12 +478,22 @@ extern "C" int bita_norm_q8(const void *d_x, int32_t x_type, int32_t m_rows, int
     hipStream_t s = (hipStream_t)stream;
     const bool db = d_delta && delta_type == BITA_BF16;
     if (x_type == BITA_BF16) {
-        if (db) launch_rows<ROWS_NORM, true, true>(a, m_rows, s);
-        else launch_rows<ROWS_NORM, true, false>(a, m_rows, s);
+        if (db) launch_rows<ROWS_NORM, true, BITA_BF16>(a, m_rows, s);
+        else launch_rows<ROWS_NORM, true, BITA_F32>(a, m_rows, s);
     } else {
-        if (db) launch_rows<ROWS_NORM, false, true>(a, m_rows, s);
-        else launch_rows<ROWS_NORM, false, false>(a, m_rows, s);
+        if (db) launch_rows<ROWS_NORM, false, BITA_BF16>(a, m_rows, s);
+        else launch_rows<ROWS_NORM, false, BITA_F32>(a, m_rows, s);
     }
+    BITA_HIP_CHECK(hipGetLastError());
+    return BITA_OK;
+}
+
+// x += the sums of a product (its d columns as many as x's, a multiple of 16), then as bita_norm_q8
+int norm_q8_of_sums(float *d_x, int m_rows, int64_t d, const SumsQ8 &delta, const void *d_gain, float eps, int8_t *d_q, int64_t ldq, float *d_scale, hipStream_t s) {
+    RowsArgs a = {};
+    a.x = d_x; a.delta = delta.part; a.sums = delta; a.sums_step = (int64_t)m_rows * d; a.gain = (const uint16_t *)d_gain; a.total = d_x; a.q = d_q; a.scale = d_scale;
+    a.ldx = a.ld_total = d; a.ldq = ldq; a.k = (int)d; a.eps = (double)eps;
+    launch_rows<ROWS_NORM, false, SUMS>(a, m_rows, s);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
 }

@@ -142,6 +142,17 @@ def test_pass_of_an_8_bit_model(cfg_name, rows, ctx, page):
         near(k[live] - k_ref[l][live], k_ref[l][live] - k_plain[l][live])
 
 
+@pytest.mark.parametrize("rows,ctx", [(8, 33), (1, 1), (40, 100)])
+def test_pass_whose_products_are_split(rows, ctx, monkeypatch):
+    """The output and down projections' k is split: the norms behind them, and at the end the LM head's, take up the sums."""
+    import paper_2401_12522_amd as bita
+    cfg = synth.get_config("tiny", d_model=256, n_heads=128, n_kv_heads=128, d_ffn=8192, n_layers=2)
+    monkeypatch.setitem(synth.configs.CONFIGS, "long sums", cfg)
+    for k in (cfg.n_heads * cfg.head_dim, cfg.d_ffn):
+        assert bita.binding.gemm_q8_plan_info(rows + cfg.n_mask, cfg.d_model, k)["splits"] > 1
+    test_pass_of_an_8_bit_model("long sums", rows, ctx, 0)
+
+
 def _greedy(model, cfg, tokens, n, tree):
     """Tokens and smallest top-2 distance of a free-running decode from a prefilled context."""
     import paper_2401_12522_amd as bita
