@@ -13,8 +13,8 @@
 // (the norm's and the gating's maximum is refined in double behind a second one: by the few threads that hold a candidate, who read
 // its sources again; held in registers they made the few rows no faster and the gating spill).  What bounds it is memory where there
 // are many rows, provided that a value costs few instructions and a row few waits: values in groups of eight a thread, one branch a
-// group for all that is rare (34, 26 and 16 vector instructions a value for norm, gating and plain rows, bf16), the waves' maxima and sums read side by side (one after the other they cost more than the row: 11008
-// rows of 4096 bf16 91 us).
+// group for all that is rare (34, 26 and 16 vector instructions a value for norm, gating and plain rows, bf16), the waves' maxima and
+// sums read side by side (one after the other they cost more than the row: 11008 rows of 4096 bf16 91 us).
 #include "common.h"
 
 enum { ROWS_PLAIN = 0, ROWS_NORM = 1, ROWS_GATE = 2 };
