@@ -344,6 +344,12 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
     constexpr int COLS = 32 * NF, LD = COLS / 4 + 1;                                  // in 16-byte pieces
     static_assert(WAVES * 32 * LD <= 2 * STAGE && (NF & (NF - 1)) == 0, "the epilogue's rows fit the stages, its lanes divide a wave");
     i32x4 *own = lds + wave * 32 * LD;
+    // between lanes' stores there and other lanes' reads, and before the next stores: a wave's LDS operations keep their order, which the compiler
+    // has to keep too (to it a lane's store and its reads are of places that may be told apart); no instruction
+    auto turned = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
     auto leave = [&](auto *o, int64_t ldo, int64_t n) __attribute__((always_inline)) {
         constexpr int V = 16 / (int)sizeof(*o), LANES = COLS / V, ROWS = 64 / LANES;  // columns of a lane, lanes of a row, rows a store
         const int c = lane % LANES;
@@ -360,6 +366,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
 #pragma unroll
                 for (int e = 0; e < 4; e++)
                     own[r * LD + j * 8 + 2 * e + half] = i32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+            turned();
 #pragma unroll
             for (int x = 0; x < 32; x += ROWS) {
                 const int in = x + lane / LANES, row = first + in;
@@ -371,6 +378,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_q8_tile_kernel(
                 }
                 if (row < m && col < n) store_row<V>(o, ldo, row, col, n, sum, sa[row], scale);
             }
+            turned();
         }
     };
     if (part) leave(part + (int64_t)blockIdx.y * m * n_tiles * 16, n_tiles * 16, n_tiles * 16);
