@@ -1,4 +1,4 @@
-"""Gating at the ends of the gates' range (GPU): gates whose exponent passes fp32, against silu(g) u in 64 bits.  Every integer has to be
+"""Gating at the ends of the gates' range (GPU): gates whose exponent passes fp32 and subnormal ones, against silu(g) u in 64 bits.  Every integer has to be
 the definition's, a scale within its one rounding to 32 bits."""
 import pytest
 import torch
@@ -34,3 +34,20 @@ def test_gates_that_are_large(dtype, top, up):
     check(q, scale, v)
     pairs = torch.stack([gate[:, :496].reshape(2, -1, 16), ups[:, :496].reshape(2, -1, 16)], 2).reshape(2, -1).contiguous()
     check(*bita.silu_mul_q8(pairs, tile=16), v[:, :496])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-45, 1e-43, 1e-41, 1e-39, 1.2e-38, 3e-38])
+@pytest.mark.parametrize("up", [1e30, 1e34, 3e38])
+def test_gates_that_are_subnormal(dtype, size, up):
+    """Half of such a gate is no longer a multiple of the smallest number, and a large up brings the product back into the ordinary range."""
+    import paper_2401_12522_amd as bita
+    g = torch.Generator(device="cuda").manual_seed(2)
+    f, t = 400, TYPES[dtype]
+    gate = size * torch.randn(3, f, device="cuda", generator=g, dtype=torch.float64)
+    ups = up * torch.rand(3, f, device="cuda", generator=g, dtype=torch.float64)
+    gate[1, ::2], ups[1, ::2] = -1 - torch.rand(f // 2, device="cuda", generator=g, dtype=torch.float64), size * up
+    gate[2, 5], ups[2, 5] = 60.0, size * up / 60
+    gate, ups = gate.float().to(t), ups.float().to(t)
+    q, scale = bita.silu_mul_q8(torch.cat([gate, ups], 1).contiguous())
+    check(q, scale, gated(gate, ups))
