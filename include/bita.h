@@ -340,7 +340,7 @@ int bita_gemm_noalloc(const void *d_a, const void *d_a_lo, int32_t m_rows, int64
  * bita_silu_mul_q8    v = silu(gate) * up of a gate/up product [M][2 d_ffn]: tile 16 = tiles of 16 gate columns, each followed
  *                     by its 16 up columns (bita_pack_weight's interleaving; d_ffn a multiple of 16), tile 0 = all gate columns
  *                     first.  1 <= d_ffn <= BITA_Q8_MAX_K
- *                     A product beyond fp32 counts as an infinity.
+ *                     A product that rounds to an infinity in fp32 counts as one.
  * A scale is rounded to fp32 (one beyond it, which only bita_norm_q8's gain can bring about, is an infinity).  All three only enqueue one kernel
  * on `stream` (one for every 2^21 rows) and may be captured. */
 int bita_quantize_rows(const void *d_x, int32_t x_type, int32_t m_rows, int64_t k, int64_t ldx, int8_t *d_q, int64_t ldq,

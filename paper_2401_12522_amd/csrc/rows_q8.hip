@@ -172,7 +172,7 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
     __shared__ uint32_t s_max[16];
     __shared__ double s_sum[16];
     __shared__ unsigned long long s_exact;
-    constexpr unsigned long long NO_NUMBER = ~0ull;
+    constexpr unsigned long long NO_NUMBER = ~0ull, BEYOND_FP32 = 0x47EFFFFFF0000000ull;      // (the latter 2^128 - 2^103, which rounds to an infinity)
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6, k = a.k;
     const char *x = (const char *)a.x + (int64_t)row * a.ldx * (XB ? 2 : 4);
     int8_t *q = a.q + (int64_t)row * a.ldq;
@@ -368,6 +368,8 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
         __syncthreads();
         top = __longlong_as_double((long long)s_exact);
         if constexpr (KIND == ROWS_NORM) bad = s_exact == NO_NUMBER;
+        // (fp32's own products may be on the other side of its end; their exact values, all taken in double there, are not)
+        else bad = s_exact >= BEYOND_FP32;
     }
     const bool none = bad || top == 0.0;                     // (not in_range)
     if (tid == 0) {

@@ -51,3 +51,22 @@ def test_gates_that_are_subnormal(dtype, size, up):
     gate, ups = gate.float().to(t), ups.float().to(t)
     q, scale = bita.silu_mul_q8(torch.cat([gate, ups], 1).contiguous())
     check(q, scale, gated(gate, ups))
+
+
+def test_products_next_to_the_end_of_fp32():
+    """A product that rounds to fp32's infinity is one, the next smaller one is a number: |v| at or above 2^128 - 2^103 or below it."""
+    import paper_2401_12522_amd as bita
+    g = torch.Generator(device="cuda").manual_seed(3)
+    m, f = 4000, 24
+    gate, ups = torch.randn(m, f, device="cuda", generator=g), torch.randn(m, f, device="cuda", generator=g)
+    gate[:, 7] = 2 + 10 * torch.rand(m, device="cuda", generator=g)
+    near = (torch.finfo(torch.float32).max / gated(gate[:, 7], torch.ones(m, device="cuda"))).float()
+    step = torch.randint(-4, 5, (m,), device="cuda", generator=g, dtype=torch.int32)
+    ups[:, 7] = (near.view(torch.int32) + step).view(torch.float32)
+    v, limit = gated(gate, ups), 2.0 ** 128 - 2.0 ** 103
+    beyond = v[:, 7] >= limit
+    assert bool(((v[:, 7] / limit - 1).abs() > 1e-14).all())                # (none where doubles could not tell)
+    assert 1000 < int(beyond.sum()) < 3000
+    q, scale = bita.silu_mul_q8(torch.cat([gate, ups], 1).contiguous())
+    assert torch.equal(torch.isnan(scale), beyond) and not q[beyond].any()
+    check(q[~beyond], scale[~beyond], v[~beyond])
