@@ -142,8 +142,10 @@ __device__ __forceinline__ T reduced(T v) {
 
 // The delta's type where it is the sums of a product
 #define SUMS 2
-// eight neighbouring ones, as the product itself would store them in fp32
+// eight neighbouring ones, as the product itself would store them in fp32: both products are rounded by themselves, wherever the compiler puts the
+// addition that follows
 __device__ __forceinline__ void load8_of_sums(const RowsArgs &a, int row, int at, float row_scale, float v[8]) {
+#pragma clang fp contract(off)
     typedef __attribute__((ext_vector_type(4))) int i32x4;
     const int *part = a.sums.part + (int64_t)row * a.k + at;
     i32x4 sum[2] = {};
