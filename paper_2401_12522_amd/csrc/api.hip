@@ -94,6 +94,7 @@ extern "C" int bita_model_create(const bita_config *cfg, const bita_weights *w, 
 }
 
 extern "C" int bita_model_create_q8(const bita_config *cfg, const bita_weights *w, const bita_scales_q8 *sc, bita_model **out) {
+    if (!out) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_model_create_q8: null argument");
     if (!sc || !sc->wqkv || !sc->wo || !sc->w_gate_up || !sc->w_down) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_model_create_q8: missing scales");
     if (cfg && ((int64_t)cfg->n_heads * cfg->head_dim > BITA_Q8_MAX_K || cfg->d_ffn > BITA_Q8_MAX_K))
         return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_model_create_q8: attention width and d_ffn at most %d", BITA_Q8_MAX_K);
