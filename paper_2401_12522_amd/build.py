@@ -66,6 +66,14 @@ def _kernel_resources(remarks):
     return res
 
 
+def _spilling_products(resources):
+    """The products' kernels are written to fit their register budget in every instantiation: a spill inside their loops is
+    silent and costs percents of a step (scratch traffic shares the vector-memory path and its wait counter with the weight
+    stream), so it fails the build instead."""
+    kernels = ("gemm_skinny_kernel", "gemm_q8_skinny_kernel", "gemm_q8_tile_kernel")
+    return sorted(k for k, v in resources.items() if v.get("scratch", 0) > 0 and any(n in k for n in kernels))
+
+
 def build_library(verbose=False, extra_flags=(), lib_path=LIB_PATH):
     """Every source is compiled to an object of its own (side by side, one process each: no
     device symbol crosses a file), then linked."""
@@ -82,12 +90,9 @@ def build_library(verbose=False, extra_flags=(), lib_path=LIB_PATH):
         resources.update(_kernel_resources(r))
     with open(os.path.join(obj_dir, tag + "_kernel_resources.json"), "w") as f:
         json.dump(resources, f, indent=1, sort_keys=True)
-    # The skinny GEMM is written to fit its register budget in every instantiation: a spill inside
-    # its loop is silent and costs percents of a step (scratch traffic shares the vector-memory
-    # path and its wait counter with the weight stream), so it fails the build instead.
-    spilled = sorted(k for k, v in resources.items() if "gemm_skinny_kernel" in k and v.get("scratch", 0) > 0)
+    spilled = _spilling_products(resources)
     if spilled:
-        raise RuntimeError("gemm_skinny_kernel instantiations that spill registers to scratch:\n  " + "\n  ".join(spilled))
+        raise RuntimeError("matrix products that spill registers to scratch:\n  " + "\n  ".join(spilled))
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", lib_path], verbose)
     return lib_path
 
