@@ -100,13 +100,12 @@ __device__ __forceinline__ void store8(void *row, int at, int n, const float v[8
         }
 }
 
-// silu(g) u = g u / (1 + exp(-g)) for g >= GATE_LOW: -g log2(e) in two words, so that the power of two is off by its own unit only; of a gate
-// limited to 100, where 1 + exp(-g) is 1 (g log2(e) of the largest ones is beyond fp32).  u is multiplied first: half of a subnormal gate would be
-// rounded to a multiple of the smallest number, and a large u bring that error back; where u / (1 + exp(-g)) is rounded so, v is below 100 * 2^-126,
-// and the rows that fp32 decides have a largest value of 1e-30 or more
+// silu(g) u = g u / (1 + exp(-g)) for g >= GATE_LOW: -g log2(e) in two words, so that the power of two is off by its own unit only.  Of a gate above
+// 2.36e38 the first word is an infinity and this no number: its row is then taken in double as a whole (a gate limited for the exponent costs every
+// value an instruction).  u is multiplied first: half of a subnormal gate would be rounded to a multiple of the smallest number, and a large u
+// bring that error back; where u / (1 + exp(-g)) is rounded so, v is below 100 * 2^-126, and the rows that fp32 decides have a largest value of 1e-30 or more.
 __device__ __forceinline__ float gated(float g, float u) {
-    const float x = __builtin_amdgcn_fmed3f(g, -100.f, 100.f);
-    const float h = -x * 1.44269504f, l = __builtin_fmaf(-x, 1.92596303e-8f, __builtin_fmaf(-x, 1.44269504f, -h));
+    const float h = -g * 1.44269504f, l = __builtin_fmaf(-g, 1.92596303e-8f, __builtin_fmaf(-g, 1.44269504f, -h));
     const float p = __builtin_amdgcn_exp2f(h), e = __builtin_fmaf(p, l * 0.693147181f, p);
     return u * __builtin_amdgcn_rcpf(1.0f + e) * g;
 }
