@@ -291,7 +291,8 @@ __global__ __launch_bounds__(1024) void rows_q8_kernel(RowsArgs a) {
     const float top32 = __uint_as_float(top_bits);
     const bool in_range = top32 >= PLAIN_RANGE_LO && top32 <= PLAIN_RANGE_HI;
     if constexpr (KIND != ROWS_PLAIN) {
-        // the largest value in double: of those that fp32 has within its error of its largest (all, where fp32 does not hold them)
+        // the largest value in double: of those that fp32 has within its error of its largest (all, where fp32 does not hold them; rows of zeros
+        // among these, at a cost: 68 gated rows of 11008 fp32 7.2 us, with one of zeros 15.0, norm of 68 rows of 8192 6.9 and 10.7)
         const float near = in_range ? top32 * (1.0f - 1e-5f) : 0.f;
         if (!in_range || __uint_as_float(mine_bits) >= near) {
             unsigned long long best = 0;
