@@ -70,3 +70,21 @@ def test_products_next_to_the_end_of_fp32():
     q, scale = bita.silu_mul_q8(torch.cat([gate, ups], 1).contiguous())
     assert torch.equal(torch.isnan(scale), beyond) and not q[beyond].any()
     check(q[~beyond], scale[~beyond], v[~beyond])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,f", [(3, 9000), (1500, 4100), (3, 20000), (3, 33000), (2, 70001)])
+def test_long_rows_with_a_large_gate(m, f, dtype):
+    """Rows of several groups of values a thread, and longer than a workgroup holds: a large gate in the last values, beside an ordinary row and an infinity."""
+    import paper_2401_12522_amd as bita
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(m, 2 * f, device="cuda", generator=g)
+    x[0, f - 2], x[0, 2 * f - 2] = 3e38, 0.25
+    if m > 2:
+        x[2, f - 1], x[2, 2 * f - 1] = float("inf"), 0.5
+    x = x.to(TYPES[dtype])
+    q, scale = bita.silu_mul_q8(x)
+    rows = [r for r in range(m) if r != 2]
+    check(q[rows], scale[rows], gated(x[rows, :f], x[rows, f:]))
+    if m > 2:
+        assert bool(torch.isnan(scale[2])) and not q[2].any()
