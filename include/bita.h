@@ -386,6 +386,90 @@ typedef struct bita_scales_q8 {
 } bita_scales_q8;
 int bita_model_create_q8(const bita_config *cfg, const bita_weights *w, const bita_scales_q8 *scales, bita_model **out);
 
+/* ---- a K/V cache in 4 or 8 bits, and the attention block around it ---------------------------------------
+ * One layer's cache as microscaled blocks: 32 neighbouring values v of a head share a power of two 2^e and are held as c = v / 2^e
+ * in 4 bits (1 sign, 2 exponent, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) or 8 (1, 4, 3: up to 448), rounded to nearest, ties to
+ * the even code.  e is the smallest integer at which no value of the block rounds past the largest c, but at least -125 (4 bits) or -117
+ * (8 bits), so that every c 2^e is a normal bf16 number or zero: what is read back is exact in bf16.  A scale byte holds e + 127; 255 marks
+ * a block that had a NaN or an infinity in it: its codes are 0 and all of it reads back as NaN.  128 values of a head take 68 or 132 bytes
+ * instead of 256.
+ *   k, v               codes [batch][n_kv_heads][smax][head_dim * bits / 8], 4-bit codes in pairs, the first in the low half of a byte
+ *   k_scale, v_scale   bytes [batch][n_kv_heads][smax][head_dim / 32]
+ * or, with a block_table as in bita_kv ([batch][max_pages]; page_size a power of two >= 16), page pools
+ *   codes [n_pages][n_kv_heads][page_size][..], scales [n_pages][n_kv_heads][page_size][..];  smax <= max_pages * page_size, and page ids are
+ * clamped to the pool (a bad table gives wrong data, never a fault).
+ * bits 4 or 8; head_dim 64 or 128; the four pointers multiples of 16 bytes. */
+typedef struct bita_kv_mx {
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+    int32_t bits, batch, n_kv_heads, head_dim, smax;
+    const int32_t *block_table;
+    int32_t page_size, n_pages, max_pages;
+} bita_kv_mx;
+
+/* Rows to blocks as the cache is written: row i < count[b] of sequence b goes to slot d_start[b] + i (rows that would lie
+ * outside 0 .. smax-1 are dropped).  d_k, d_v: BITA_BF16 or BITA_F32, of head h, row r of sequence b the head_dim values at
+ * b * seq + h * head + r * row (strides k_* and v_* in elements, multiples of 8; pointers multiples of 16 bytes).
+ *   n_rows    rows of a sequence in d_k, d_v; packed: of all sequences together
+ *   d_count   [batch] or NULL: rows to write, of at most n_rows (path_stride with a path; packed: the sequence's own rows); NULL: all of them
+ *   d_path    [batch][path_stride] or NULL: row i is taken from row path[b][i] (clamped), as bita_compact_kv takes accepted rows
+ *   d_cu_rows [batch+1] or NULL: packed rows: sequence b's are rows cu[b] .. cu[b+1]-1 of one axis (the seq strides are not used, d_path is NULL);
+ *             rows outside all of them are left out
+ * bita_kv_read_mx is the way back: slot d_start[b] + i, i < min(d_length[b], n_slots), of head h to out_type values at
+ * b * seq + h * head + i * row of d_k and d_v (either may be NULL); slots outside 0 .. smax-1 and everything
+ * behind a sequence's length are left as they are.  d_start NULL: 0.  Neither changes a length.  One kernel each; may be captured. */
+int bita_kv_write_mx(const bita_kv_mx *kv, const void *d_k, int64_t k_seq, int64_t k_head, int64_t k_row, const void *d_v, int64_t v_seq, int64_t v_head,
+                     int64_t v_row, int32_t type, int32_t n_rows, const int32_t *d_start, const int32_t *d_count, const int32_t *d_path, int32_t path_stride,
+                     const int32_t *d_cu_rows, void *stream);
+int bita_kv_read_mx(const bita_kv_mx *kv, void *d_k, int64_t k_seq, int64_t k_head, int64_t k_row, void *d_v, int64_t v_seq, int64_t v_head, int64_t v_row,
+                    int32_t out_type, int32_t n_slots, const int32_t *d_start, const int32_t *d_length, void *stream);
+
+/* Queries and keys of a QKV product [M][(n_heads + 2 n_kv_heads) * head_dim] ready for attention: every head h of q and k becomes
+ * h / sqrt(mean(h^2) + eps) * gain (gains bf16 [head_dim]; NULL: as it is), then its pairs (i, i + head_dim/2) are rotated by the angle whose cosine and sine are
+ * d_cos, d_sin [max_pos][head_dim/2] at d_pos[m] (clamped to the table); v is copied.  In fp32, rounded once to bf16.
+ *   d_x BITA_F32 or BITA_BF16, rows ldx elements apart; d_q, d_k, d_v (d_v may be NULL: v is left out) bf16, row m, head h at
+ *   m * ld + h * head_stride.  Strides are multiples of 8 elements, pointers (gains and tables too) of 16 bytes.  head_dim 64 or 128; eps finite and >= 0.
+ *   The outputs may be the columns of d_x that they are computed from (bf16); otherwise nothing overlaps.  One kernel; may be captured. */
+int bita_qk_norm_rope(const void *d_x, int32_t x_type, int32_t m_rows, int64_t ldx, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                      const void *d_q_gain, const void *d_k_gain, float eps, const int32_t *d_pos, const float *d_cos, const float *d_sin, int32_t max_pos,
+                      void *d_q, int64_t ldq, int64_t q_head_stride, void *d_k, int64_t ldk, int64_t k_head_stride,
+                      void *d_v, int64_t ldv, int64_t v_head_stride, void *stream);
+
+/* bita_tree_attention over such a cache: every row of the pass attends to the prompt prefix (mask rows only), to slots
+ * 0 .. ctx_len[b]-1 of the cache and to its ancestors-or-self among the rows of the pass (a template of one row: one token).
+ *   d_q    bf16 [B][R][n_heads][hd], contiguous
+ *   d_k_rows, d_v_rows  bf16, of head h, row r of sequence b the hd values at b * seq + h * head + r * row (strides k_* and v_* in
+ *          elements, multiples of 8): the rows' K/V, not yet in the cache
+ *   d_prompt_k, d_prompt_v  bf16 [n_kv_heads][n_prompt][hd] or NULL with n_prompt 0
+ *   d_ctx_len [B] (read as at most ctx_hint and smax);  ctx_hint: HOST upper bound of them, at most smax
+ *   d_token   [B][R] or NULL: a tree row with a negative token is absent and its output zero (it stays visible to the rows below it)
+ *   d_out  bf16 [B][R][n_heads * hd];  d_ws: bita_tree_attention_mx_workspace_bytes(), a multiple of 16, nothing in it kept from call to call, calls that
+ *          may run at the same time have each their own.  The pointers of bf16 tensors are multiples of 16 bytes.
+ * Any n_heads that is a multiple of n_kv_heads.  One kernel, or two where the keys are split; may be captured.  Scores, sums and
+ * accumulation are fp32; probabilities go to the matrix product as bf16.
+ * bita_tree_attention_mx_plan_info: how it is cut (for tests and reports): out4 (HOST) = {key splits, queries of a workgroup, waves of a
+ * workgroup, workgroups}. */
+size_t bita_tree_attention_mx_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t bits,
+                                              int32_t ctx_hint, int32_t n_prompt);
+int bita_tree_attention_mx_plan_info(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t bits, int32_t ctx_hint,
+                                     int32_t n_prompt, int32_t *out4);
+int bita_tree_attention_mx(const bita_tree_template *t, const void *d_q, const bita_kv_mx *kv, const void *d_k_rows, int64_t k_seq, int64_t k_head,
+                           int64_t k_row, const void *d_v_rows, int64_t v_seq, int64_t v_head, int64_t v_row, const void *d_prompt_k, const void *d_prompt_v,
+                           int32_t n_prompt, const int32_t *d_ctx_len, const int32_t *d_token, int32_t n_heads, int32_t ctx_hint, void *d_ws,
+                           size_t ws_bytes, void *d_out, void *stream);
+
+/* Causal attention over whole prompts packed one behind the other: token i of sequence b (rows cu[b] .. cu[b+1]-1) attends to the
+ * sequence's tokens 0 .. i.  For the pass over the input that precedes the first draft, without a limit on rows and without chunks.
+ *   d_q, d_k, d_v  bf16, token t, head h at t * ld + h * head_stride (elements; multiples of 8, pointers of 16 bytes): tensors of
+ *                  their own, or columns of one QKV product
+ *   d_cu_seqlens   [n_seqs + 1], device, not decreasing, between 0 and n_tokens (clamped; sequences may be empty)
+ *   d_out          bf16 rows of n_heads * head_dim, ldo apart; rows outside all sequences are left as they are
+ * head_dim 64 or 128, any n_heads that is a multiple of n_kv_heads.  Scores, sums and accumulation are fp32; probabilities go to the matrix
+ * product as bf16.  One kernel; may be captured. */
+int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_head_stride, const void *d_k, int64_t ldk, int64_t k_head_stride, const void *d_v,
+                          int64_t ldv, int64_t v_head_stride, const int32_t *d_cu_seqlens, int32_t n_seqs, int32_t n_tokens, int32_t n_heads,
+                          int32_t n_kv_heads, int32_t head_dim, void *d_out, int64_t ldo, void *stream);
+
 /* Measurement aid: while enabled, bita_verify_step brackets each of its GEMM launches with
  * a pair of HIP events on the caller's stream (not usable under graph capture).
  * bita_profile_enable creates the events (up to max_records launches are recorded from the

@@ -22,6 +22,8 @@ EXPORTS = [
     "bita_profile_disable", "bita_profile_read", "bita_last_error",
     "bita_quantize_rows", "bita_norm_q8", "bita_silu_mul_q8", "bita_packed_q8_bytes", "bita_pack_weight_q8",
     "bita_model_create_q8", "bita_gemm_q8_workspace_bytes", "bita_gemm_q8_plan_info", "bita_gemm_q8",
+    "bita_kv_write_mx", "bita_kv_read_mx", "bita_qk_norm_rope", "bita_tree_attention_mx_workspace_bytes", "bita_tree_attention_mx_plan_info",
+    "bita_tree_attention_mx", "bita_prompt_attention",
 ]
 
 
@@ -50,6 +52,12 @@ class _ScalesQ8(C.Structure):
 class _KV(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k_cache", "v_cache", "k_tree", "v_tree")] + \
                [(n, C.c_int32) for n in ("smax", "rows", "batch", "ctx_hint")] + \
+               [("block_table", C.c_void_p)] + [(n, C.c_int32) for n in ("page_size", "n_pages", "max_pages")]
+
+
+class _KVMX(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + \
+               [(n, C.c_int32) for n in ("bits", "batch", "n_kv_heads", "head_dim", "smax")] + \
                [("block_table", C.c_void_p)] + [(n, C.c_int32) for n in ("page_size", "n_pages", "max_pages")]
 
 
@@ -122,6 +130,19 @@ def lib():
     L.bita_gemm_q8_workspace_bytes.restype, L.bita_gemm_q8_workspace_bytes.argtypes = sz, [i32, i64, i64]
     L.bita_gemm_q8_plan_info.restype, L.bita_gemm_q8_plan_info.argtypes = C.c_int, [i32, i64, i64, vp]
     L.bita_gemm_q8.restype, L.bita_gemm_q8.argtypes = C.c_int, [vp, i64, vp, i32, i64, vp, vp, i64, vp, sz, vp, i32, i64, vp]
+    kvp = C.POINTER(_KVMX)
+    L.bita_kv_write_mx.restype = C.c_int
+    L.bita_kv_write_mx.argtypes = [kvp, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, vp, vp, vp, i32, vp, vp]
+    L.bita_kv_read_mx.restype = C.c_int
+    L.bita_kv_read_mx.argtypes = [kvp, vp, i64, i64, i64, vp, i64, i64, i64, i32, i32, vp, vp, vp]
+    L.bita_qk_norm_rope.restype = C.c_int
+    L.bita_qk_norm_rope.argtypes = [vp, i32, i32, i64, i32, i32, i32, vp, vp, C.c_float, vp, vp, vp, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp]
+    L.bita_tree_attention_mx_workspace_bytes.restype, L.bita_tree_attention_mx_workspace_bytes.argtypes = sz, [i32] * 8
+    L.bita_tree_attention_mx_plan_info.restype, L.bita_tree_attention_mx_plan_info.argtypes = C.c_int, [i32] * 8 + [vp]
+    L.bita_tree_attention_mx.restype = C.c_int
+    L.bita_tree_attention_mx.argtypes = [vp, vp, kvp, vp, i64, i64, i64, vp, i64, i64, i64, vp, vp, i32, vp, vp, i32, i32, vp, sz, vp, vp]
+    L.bita_prompt_attention.restype = C.c_int
+    L.bita_prompt_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i32, i32, i32, i32, i32, vp, i64, vp]
     _lib = L
     return L
 
@@ -696,6 +717,226 @@ def gemm_q8(a, a_scale, w_packed, w_scale, n_rows, out=None, out_dtype=torch.flo
         pw = workspace.data_ptr()
     rc = L.bita_gemm_q8(pa, lda, a_scale.data_ptr(), m, k, w_packed.data_ptr(), w_scale.data_ptr(), n_rows, pw, nw, out.data_ptr(), _F32_BF16[out.dtype],
                         ldo, _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return out
+
+
+# ---- a K/V cache in 4 or 8 bits, and the attention block around it ------------------------------------------------------------
+_BF16 = {torch.bfloat16: 1}
+
+
+def _tensor(name, t, types, dev, shape):
+    """Strides of t, a tensor of one of these types and this shape (None: any extent) on the current device, neighbouring elements last."""
+    if t.dtype in types and t.get_device() == dev and t.dim() == len(shape):
+        for have, want in zip(t.shape, shape):
+            if want is not None and have != want:
+                break
+        else:
+            s = t.stride()
+            if s[-1] == 1:
+                return s if 1 not in t.shape else tuple(0 if n == 1 else st for n, st in zip(t.shape, s))
+    raise ValueError(f"{name}: wanted {' x '.join('any' if n is None else str(n) for n in shape)} of {' or '.join(str(x) for x in types)} on cuda:{dev}, "
+                     f"last dimension contiguous; got {tuple(t.shape)} of {t.dtype} on {t.device}, strides {tuple(t.stride())}")
+
+
+def _dense(name, t, types, dev, shape):
+    _tensor(name, t, types, dev, shape)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: wanted a contiguous tensor; got strides {tuple(t.stride())}")
+
+
+_I32, _U8, _F32 = {torch.int32: 0}, {torch.uint8: 0}, {torch.float32: 0}
+
+
+class KVCacheMX:
+    """One layer's K/V cache as microscaled blocks of 32 values in 4 or 8 bits (head_dim 64 or 128): 68 or 132 bytes a row of 128 values instead
+    of 256.  Contiguous [batch][n_kv_heads][smax], or with a block_table (int32 cuda [batch][max_pages]) pools of
+    [n_pages][n_kv_heads][page_size].  k, v (codes, uint8) and k_scale, v_scale (uint8) are allocated here where they are not given.  The
+    caller keeps the sequences' lengths, as KVState.ctx_len does."""
+
+    def __init__(self, n_kv_heads, head_dim, batch, smax, bits=4, block_table=None, page_size=0, n_pages=None, k=None, v=None, k_scale=None, v_scale=None):
+        dev = torch.cuda.current_device()
+        self.n_kv_heads, self.head_dim, self.batch, self.smax, self.bits = int(n_kv_heads), int(head_dim), int(batch), int(smax), int(bits)
+        if self.bits not in (4, 8) or self.head_dim not in (64, 128) or min(self.n_kv_heads, self.batch, self.smax) < 1:
+            raise ValueError(f"KVCacheMX: bits 4 or 8, head_dim 64 or 128 and positive sizes wanted; got {bits}, {head_dim}, {(n_kv_heads, batch, smax)}")
+        self.block_table, self.page_size, self.max_pages, self.n_pages = block_table, 0, 0, 0
+        if block_table is not None:
+            _dense("block_table", block_table, _I32, dev, (self.batch, None))
+            self.page_size, self.max_pages = int(page_size), block_table.shape[1]
+            if self.page_size < 16 or self.page_size & (self.page_size - 1) or self.smax > self.max_pages * self.page_size:
+                raise ValueError(f"KVCacheMX: page_size a power of two >= 16 and smax <= {self.max_pages} pages of it wanted; got {page_size}, {smax}")
+            self.n_pages = int(n_pages) if n_pages is not None else k.shape[0] if k is not None else self.batch * self.max_pages
+        rows = (self.n_pages, self.n_kv_heads, self.page_size) if block_table is not None else (self.batch, self.n_kv_heads, self.smax)
+        for name, t, width in (("k", k, self.head_dim * self.bits // 8), ("v", v, self.head_dim * self.bits // 8), ("k_scale", k_scale, self.head_dim // 32),
+                               ("v_scale", v_scale, self.head_dim // 32)):
+            if t is None:
+                t = torch.zeros(rows + (width,), dtype=torch.uint8, device="cuda") if width > 4 else torch.full(rows + (width,), 127, dtype=torch.uint8, device="cuda")
+            _dense(name, t, _U8, dev, rows + (width,))
+            setattr(self, name, t)
+        self._device = dev
+        self._desc = _KVMX(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(), self.bits, self.batch, self.n_kv_heads,
+                           self.head_dim, self.smax, block_table.data_ptr() if block_table is not None else None, self.page_size, self.n_pages, self.max_pages)
+        self._ref = C.byref(self._desc)
+
+    def on(self, dev):
+        """The descriptor, for a call on device dev."""
+        if dev != self._device:
+            raise ValueError(f"the cache is on cuda:{self._device}, the current device is cuda:{dev}")
+        return self._ref
+
+
+def kv_write_mx(cache, k, v, start, count=None, path=None, cu_rows=None):
+    """Rounds rows to blocks as they are written to the cache: row i of sequence b to slot start[b] + i (rows that would lie outside the cache are
+    dropped).  k, v: cuda float32 or bfloat16, [B][Hkv][n][hd] as tree_attention's pass rows, or with cu_rows
+    (int32 [B+1]) packed [T][Hkv][hd].  start, count: int32 [B]; count None: all rows.  path int32 [B][m]: row i is k[b, :, path[b, i]]
+    (accept's path, with count its n_acc).  No length is changed."""
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    ref, B, H, D = cache.on(dev), cache.batch, cache.n_kv_heads, cache.head_dim
+    seq = vseq = 0
+    if cu_rows is not None:
+        n = k.shape[0]
+        row, head, _ = _tensor("k", k, _F32_BF16, dev, (None, H, D))
+        vrow, vhead, _ = _tensor("v", v, {k.dtype: 0}, dev, (n, H, D))
+        _vector("cu_rows", cu_rows, B + 1, torch.int32, dev)
+    else:
+        seq, head, row, _ = _tensor("k", k, _F32_BF16, dev, (B, H, None, D))
+        n = k.shape[2]
+        vseq, vhead, vrow, _ = _tensor("v", v, {k.dtype: 0}, dev, (B, H, n, D))
+    _vector("start", start, B, torch.int32, dev)
+    if count is not None:
+        _vector("count", count, B, torch.int32, dev)
+    if path is not None:
+        _dense("path", path, _I32, dev, (B, None))
+    rc = L.bita_kv_write_mx(ref, k.data_ptr(), seq, head, row, v.data_ptr(), vseq, vhead, vrow, _F32_BF16[k.dtype], n, start.data_ptr(), count.data_ptr() if count is not None else None,
+                            path.data_ptr() if path is not None else None, path.shape[1] if path is not None else 0,
+                            cu_rows.data_ptr() if cu_rows is not None else None, _raw_stream(dev))
+    if rc:
+        _check(rc)
+
+
+def kv_read_mx(cache, k, v, length, start=None):
+    """The way back: slot start[b] + i of the cache, i < min(length[b], n), to k[b, :, i] and v[b, :, i] (cuda bfloat16 or float32 [B][Hkv][n][hd];
+    exact in either; one of them may be None).  start, length: int32 [B]; start None: 0.  What lies behind a length is left as it is."""
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    ref, one = cache.on(dev), k if k is not None else v
+    seq, head, row, _ = vseq, vhead, vrow, _ = _tensor("k" if k is not None else "v", one, _F32_BF16, dev, (cache.batch, cache.n_kv_heads, None, cache.head_dim))
+    if v is not None and k is not None:
+        vseq, vhead, vrow, _ = _tensor("v", v, {k.dtype: 0}, dev, k.shape)
+    _vector("length", length, cache.batch, torch.int32, dev)
+    if start is not None:
+        _vector("start", start, cache.batch, torch.int32, dev)
+    rc = L.bita_kv_read_mx(ref, k.data_ptr() if k is not None else None, seq, head, row, v.data_ptr() if v is not None else None, vseq, vhead, vrow,
+                           _F32_BF16[one.dtype], one.shape[2], start.data_ptr() if start is not None else None, length.data_ptr(), _raw_stream(dev))
+    if rc:
+        _check(rc)
+
+
+def qk_norm_rope(x, pos, cos, sin, n_heads, n_kv_heads, q_gain=None, k_gain=None, eps=1e-5, q=None, k=None, v=None):
+    """Queries and keys of a QKV product x (cuda [M][(n_heads + 2 n_kv_heads) * hd], float32 or bfloat16) ready for attention: RMSNorm of every head with a gain
+    (bfloat16 [hd]; None: no norm), rotation of its pairs (i, i + hd/2) by the angles of pos[m] (cos, sin: float32 [max_pos][hd/2]).
+    Returns (q [M][n_heads][hd], k [M][n_kv_heads][hd], v) in bfloat16, written into q, k, v where they are given (they may be views of a
+    bfloat16 x's own columns).  v: x's rounded to bfloat16; where x is bfloat16 and no v is given, a view of x."""
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    max_pos, half = cos.shape
+    hd = 2 * half
+    m, _, ldx = _matrix("x", x, _F32_BF16, dev, None, (n_heads + 2 * n_kv_heads) * hd)
+    _dense("cos", cos, _F32, dev, (None, None))
+    _dense("sin", sin, _F32, dev, (max_pos, half))
+    _vector("pos", pos, m, torch.int32, dev)
+    for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
+        if t is not None:
+            _vector(name, t, hd, torch.bfloat16, dev)
+    q = torch.empty((m, n_heads, hd), dtype=torch.bfloat16, device=x.device) if q is None else q
+    k = torch.empty((m, n_kv_heads, hd), dtype=torch.bfloat16, device=x.device) if k is None else k
+    (ldq, hq, _), (ldk, hk, _) = _tensor("q", q, _BF16, dev, (m, n_heads, hd)), _tensor("k", k, _BF16, dev, (m, n_kv_heads, hd))
+    pv = ldv = hv = 0
+    if v is None and x.dtype is torch.bfloat16:
+        v = x[:, (n_heads + n_kv_heads) * hd:].unflatten(1, (n_kv_heads, hd))
+    else:
+        v = torch.empty((m, n_kv_heads, hd), dtype=torch.bfloat16, device=x.device) if v is None else v
+        ldv, hv, _ = _tensor("v", v, _BF16, dev, (m, n_kv_heads, hd))
+        pv = v.data_ptr()
+    rc = L.bita_qk_norm_rope(x.data_ptr(), _F32_BF16[x.dtype], m, ldx, n_heads, n_kv_heads, hd, q_gain.data_ptr() if q_gain is not None else None,
+                             k_gain.data_ptr() if k_gain is not None else None, eps, pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), max_pos, q.data_ptr(), ldq, hq,
+                             k.data_ptr(), ldk, hk, pv, ldv, hv, _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return q, k, v
+
+
+@functools.lru_cache(4096)
+def _attention_mx_scratch(*sizes):
+    return lib().bita_tree_attention_mx_workspace_bytes(*sizes)
+
+
+def tree_attention_mx_plan_info(batch, rows, heads, kv_heads, head_dim, bits, ctx_hint, n_prompt=0):
+    """{splits (of the keys), queries, waves (of a workgroup), workgroups} that tree_attention_mx of these sizes launches."""
+    out = (C.c_int32 * 4)()
+    _check(lib().bita_tree_attention_mx_plan_info(batch, rows, heads, kv_heads, head_dim, bits, int(ctx_hint), n_prompt, out))
+    return dict(splits=out[0], queries=out[1], waves=out[2], workgroups=out[3])
+
+
+def tree_attention_mx(tmpl, q, cache, k_rows, v_rows, ctx_len, ctx_hint, prompt_k=None, prompt_v=None, token=None, out=None, workspace=None):
+    """tree_attention over a KVCacheMX: q bfloat16 [B][R][Hq][hd]; k_rows, v_rows bfloat16 [B][Hkv][R][hd] (any strides): the pass' rows, not in
+    the cache yet; ctx_len int32 [B], at most ctx_hint; prompt_k/v bfloat16 [Hkv][P][hd] or None; token int32 [B][R] or None (tree rows with
+    a negative token are absent, their output zero).  Returns bfloat16 [B][R][Hq*hd], written into out where it is given.
+    workspace: uint8 cuda of bita_tree_attention_mx_workspace_bytes (allocated here when it is None and one is needed)."""
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    ref, B, H, D, R = cache.on(dev), cache.batch, cache.n_kv_heads, cache.head_dim, tmpl.rows
+    _dense("q", q, _BF16, dev, (B, R, None, D))
+    Hq, ctx_hint = q.shape[2], int(ctx_hint)
+    seq, head, row, _ = _tensor("k_rows", k_rows, _BF16, dev, (B, H, R, D))
+    vseq, vhead, vrow, _ = _tensor("v_rows", v_rows, _BF16, dev, (B, H, R, D))
+    P = pk = pv = 0
+    if prompt_k is not None:
+        P = prompt_k.shape[1]
+        _dense("prompt_k", prompt_k, _BF16, dev, (H, None, D))
+        _dense("prompt_v", prompt_v, _BF16, dev, (H, P, D))
+        pk, pv = prompt_k.data_ptr(), prompt_v.data_ptr()
+    _vector("ctx_len", ctx_len, B, torch.int32, dev)
+    if token is not None:
+        _dense("token", token, _I32, dev, (B, R))
+    if out is None:
+        out = torch.empty((B, R, Hq * D), dtype=torch.bfloat16, device=q.device)
+    else:
+        _dense("out", out, _BF16, dev, (B, R, Hq * D))
+    pw = nw = 0
+    if workspace is None:
+        nw = _attention_mx_scratch(B, R, Hq, H, D, cache.bits, ctx_hint, P)
+        if nw:
+            workspace = torch.empty(nw, dtype=torch.uint8, device=q.device)
+    else:
+        _bytes("workspace", workspace, 0, dev)
+        nw = workspace.numel()
+    if nw:
+        pw = workspace.data_ptr()
+    rc = L.bita_tree_attention_mx(tmpl.handle, q.data_ptr(), ref, k_rows.data_ptr(), seq, head, row, v_rows.data_ptr(), vseq, vhead, vrow, pk, pv, P, ctx_len.data_ptr(),
+                                  token.data_ptr() if token is not None else None, Hq, ctx_hint, pw, nw, out.data_ptr(), _raw_stream(dev))
+    if rc:
+        _check(rc)
+    return out
+
+
+def prompt_attention(q, k, v, cu_seqlens, out=None):
+    """Causal attention over packed prompts: q bfloat16 [T][Hq][hd], k, v bfloat16 [T][Hkv][hd] (any strides: columns of one QKV product, or tensors of their
+    own); sequence b is rows cu_seqlens[b] .. cu_seqlens[b+1]-1 (int32 cuda [B+1]).  Returns bfloat16 [T][Hq*hd], written into out where it is
+    given; rows outside the sequences are left as they are (undefined where out is allocated here)."""
+    L, dev = _lib or lib(), torch.cuda.current_device()
+    ldq, hq, _ = _tensor("q", q, _BF16, dev, (None, None, None))
+    T, Hq, D = q.shape
+    ldk, hk, _ = _tensor("k", k, _BF16, dev, (T, None, D))
+    H = k.shape[1]
+    ldv, hv, _ = _tensor("v", v, _BF16, dev, (T, H, D))
+    n = cu_seqlens.numel()
+    _vector("cu_seqlens", cu_seqlens, n, torch.int32, dev)
+    if out is None:
+        out = torch.empty((T, Hq * D), dtype=torch.bfloat16, device=q.device)
+    ldo = _tensor("out", out, _BF16, dev, (T, Hq * D))[0]
+    if T == 1:
+        ldo = Hq * D
+    rc = L.bita_prompt_attention(q.data_ptr(), ldq, hq, k.data_ptr(), ldk, hk, v.data_ptr(), ldv, hv, cu_seqlens.data_ptr(), n - 1, T, Hq, H, D, out.data_ptr(),
+                                 ldo, _raw_stream(dev))
     if rc:
         _check(rc)
     return out

@@ -8,7 +8,8 @@ import sys
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libbita.so")
-SOURCES = ["api.hip", "gemm.hip", "attention.hip", "misc.hip", "tree.hip", "prefill.hip", "rows_q8.hip", "gemm_q8.hip"]
+SOURCES = ["api.hip", "gemm.hip", "attention.hip", "misc.hip", "tree.hip", "prefill.hip", "rows_q8.hip", "gemm_q8.hip",
+           "norm_rope.hip", "kv_mx.hip", "attention_mx.hip", "prompt_attention.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -67,10 +68,10 @@ def _kernel_resources(remarks):
 
 
 def _spilling_products(resources):
-    """The products' kernels are written to fit their register budget in every instantiation: a spill inside their loops is
+    """The products' kernels, and those of the small cache's and the prompts' attention, are written to fit their register budget in every instantiation: a spill inside their loops is
     silent and costs percents of a step (scratch traffic shares the vector-memory path and its wait counter with the weight
     stream), so it fails the build instead."""
-    kernels = ("gemm_skinny_kernel", "gemm_q8_skinny_kernel", "gemm_q8_tile_kernel")
+    kernels = ("gemm_skinny_kernel", "gemm_q8_skinny_kernel", "gemm_q8_tile_kernel", "attn_mx_kernel", "prompt_attn_kernel")
     return sorted(k for k, v in resources.items() if v.get("scratch", 0) > 0 and any(n in k for n in kernels))
 
 
@@ -92,7 +93,7 @@ def build_library(verbose=False, extra_flags=(), lib_path=LIB_PATH):
         json.dump(resources, f, indent=1, sort_keys=True)
     spilled = _spilling_products(resources)
     if spilled:
-        raise RuntimeError("matrix products that spill registers to scratch:\n  " + "\n  ".join(spilled))
+        raise RuntimeError("kernels that spill registers to scratch:\n  " + "\n  ".join(spilled))
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", lib_path], verbose)
     return lib_path
 

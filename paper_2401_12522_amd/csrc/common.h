@@ -80,6 +80,23 @@ int  bita_set_error(int code, const char *fmt, ...);
             return bita_set_error(BITA_ERR_HIP, "%s failed: %s", #expr, hipGetErrorString(_e)); \
     } while (0)
 
+// Whether rows of `width` elements in a tensor of up to three axes (extents, strides) may overlap: an axis, taken from the smallest stride up, has to
+// step past everything that the ones before it span.  For outputs, whose rows are written in no order.
+struct Axis { int64_t n, stride; };
+inline bool rows_overlap(int64_t width, Axis a, Axis b, Axis c = {1, 0}) {
+    Axis ax[3] = {a, b, c};
+    for (int i = 0; i < 2; i++)
+        for (int j = 0; j < 2 - i; j++)
+            if (ax[j].stride > ax[j + 1].stride) { const Axis t = ax[j]; ax[j] = ax[j + 1]; ax[j + 1] = t; }
+    __int128 span = width;
+    for (const Axis &x : ax)
+        if (x.n > 1) {
+            if (x.stride < span) return true;
+            span += (__int128)(x.n - 1) * x.stride;
+        }
+    return false;
+}
+
 // ---- device mirror of a pass layout ---------------------------------------------
 struct TemplateDev {
     int32_t rows, n_tree, n_mask, n_groups, depth_max, kmax, words;
