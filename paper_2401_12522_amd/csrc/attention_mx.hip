@@ -298,7 +298,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
                     const f32x4 n_up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
                     const f32x4 n_down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-                    for (int r = 0; r < 4; r++) o[u][n][r] += nonfinite_term(n_up[r], n_down[r]);
+                    for (int r = 0; r < 4; r++) o[u][n][r] += nonfinite_term(n_up[r]) - nonfinite_term(n_down[r]);
                 }
                 o[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf, o[u][n], 0, 0, 0);
             }

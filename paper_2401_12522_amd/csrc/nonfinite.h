@@ -10,20 +10,36 @@ __device__ __forceinline__ bool has_nonfinite(bf16x8 v) {
     const uint4 u = __builtin_bit_cast(uint4, v);
     return (nonfinite_halves(u.x) | nonfinite_halves(u.y) | nonfinite_halves(u.z) | nonfinite_halves(u.w)) != 0;
 }
-// v without its infinities and NaN; up: 1 where v is +inf or NaN; down: 1 where it is -inf or NaN
-__device__ __forceinline__ void split_nonfinite(bf16x8 &v, bf16x8 &up, bf16x8 &down) {
-    typedef __attribute__((ext_vector_type(8))) uint16_t u8;
-    u8 x = __builtin_bit_cast(u8, v), a, b;
+// v without its infinities and NaN; not 0 if there were any
+__device__ __forceinline__ uint32_t drop_nonfinite(bf16x8 &v) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+    u4 x = __builtin_bit_cast(u4, v);
+    uint32_t any = 0;
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-        const bool bad = (x[e] & 0x7F80) == 0x7F80, nan = bad && (x[e] & 0x7F);
-        a[e] = bad && (nan || !(x[e] & 0x8000)) ? 0x3F80 : 0;
-        b[e] = bad && (nan || (x[e] & 0x8000)) ? 0x3F80 : 0;
-        x[e] = bad ? 0 : x[e];
+    for (int i = 0; i < 4; i++) {
+        const uint32_t bad = nonfinite_halves(x[i]);
+        x[i] &= ~((bad >> 15) * 0xFFFFu);
+        any |= bad;
+    }
+    v = __builtin_bit_cast(bf16x8, x);
+    return any;
+}
+// v without its infinities and NaN; up: 1 where v is +inf or NaN; down: 1 where it is -inf or NaN.  (Two halves a word at a time: compares of
+// single values would take a pair of scalar registers each.)
+__device__ __forceinline__ void split_nonfinite(bf16x8 &v, bf16x8 &up, bf16x8 &down) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+    u4 x = __builtin_bit_cast(u4, v), a, b;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t w = x[i], bad = nonfinite_halves(w), nan = ((((w & 0x007F007Fu) + 0x007F007Fu) & 0x00800080u) << 8) & bad;
+        a[i] = ((nan | (bad & ~w)) >> 15 & 0x00010001u) * 0x3F80u;
+        b[i] = ((nan | (bad & w)) >> 15 & 0x00010001u) * 0x3F80u;
+        x[i] = w & ~((bad >> 15) * 0xFFFFu);
     }
     v = __builtin_bit_cast(bf16x8, x);
     up = __builtin_bit_cast(bf16x8, a);
     down = __builtin_bit_cast(bf16x8, b);
 }
-// what the counts of visible +inf and -inf (a NaN is both) add to a sum
-__device__ __forceinline__ float nonfinite_term(float up, float down) { return (up > 0.f ? INFINITY : 0.f) + (down > 0.f ? -INFINITY : 0.f); }
+// What a count of visible infinities adds to a sum (a NaN is both +inf and -inf, which together are one): 0 or an infinity.  (Not by a product:
+// fused with the sum it would stay finite.)
+__device__ __forceinline__ float nonfinite_term(float count) { return ldexpf(count, 255); }

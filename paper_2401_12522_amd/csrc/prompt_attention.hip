@@ -9,14 +9,13 @@
 //    barrier a tile.  Rows are swizzled by 16-byte columns on the way (by where a lane fetches from: LDS takes them in lane order),
 //    K is read back by rows, V by transposed reads.
 //  * Key tiles before a wave's queries need no mask.  Workgroups start with the longest walks.
-#include "nonfinite.h"
 #include <cmath>
+#include <type_traits>
+#include "attention_core.h"
 
 #define PA_WAVES 4
-#define PA_KEYS 64
 #define PA_ROWS (32 * PA_WAVES)
-
-typedef __attribute__((ext_vector_type(16))) float f32x16;
+#define PA_MAX_LD (1 << 24)            // offsets inside a tile of 64 rows have 32 bits (signed)
 
 struct PromptArgs {
     const uint16_t *q, *k, *v;
@@ -26,20 +25,6 @@ struct PromptArgs {
     float scale_log2;
     uint16_t *out;
 };
-
-__device__ __forceinline__ float pa_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ uint32_t pa_pk_bf16(float a, float b) {
-    typedef __attribute__((ext_vector_type(2))) float f2;
-    typedef __attribute__((ext_vector_type(2))) __bf16 b2;
-    const f2 v = {a, b};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
-}
-// the other half wave's value
-__device__ __forceinline__ float pa_other_half(float x) {
-    typedef __attribute__((ext_vector_type(2))) unsigned u2;
-    const u2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
-}
 
 // The tile's sequence, its first token and length, and the tile's number inside it, from the sequences' ends: tiles are counted over
 // the sequences, 64 of them a step.  false: no such tile.
@@ -74,141 +59,113 @@ __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &star
 
 template <int HD>
 __global__ __launch_bounds__(PA_WAVES * 64, 2) void prompt_attn_kernel(PromptArgs a) {
-    constexpr int KS = HD / 16, NT = HD / 32, GPR = HD / 8, RPI = 64 / GPR;             // k-steps, head tiles, granules a row, rows a load instruction
-    constexpr int TILE = PA_KEYS * HD * 2, LOADS = PA_KEYS / RPI / PA_WAVES;            // bytes of a K (or V) tile; load instructions a wave
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];                // [2][K | V]
+    using Core = AttnCore<HD>;
+    constexpr int KS = Core::KS, NT = Core::NT, TILE = Core::TILE, GPR = HD / 8, RPI = 64 / GPR;    // granules a row, rows a load instruction
+    constexpr int LOADS = CORE_KEYS / RPI / PA_WAVES;                                   // load instructions of a wave, K or V tile
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];                // K tiles [2], V tiles [2]
     const int lane = threadIdx.x & 63, hf = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j = blockIdx.x % a.Hq;
     const int head = a.Hq % 8 == 0 ? (j & 7) * (a.Hq >> 3) + (j >> 3) : j;              // an XCD (ids go round) takes neighbouring heads
     int start, len, tile;
     if (!pa_find(a, blockIdx.x / a.Hq, start, len, tile)) return;
-    tile = (len + PA_ROWS - 1) / PA_ROWS - 1 - tile;                                    // the longest walk first
+    start = __builtin_amdgcn_readfirstlane(start);                                      // (the same in all lanes, which the compiler cannot know)
+    len = __builtin_amdgcn_readfirstlane(len);
+    tile = (len + PA_ROWS - 1) / PA_ROWS - 1 - __builtin_amdgcn_readfirstlane(tile);    // the longest walk first
     const int q0 = tile * PA_ROWS + wave * 32, qi = q0 + c, kvh = head / a.qpk;         // of the wave, of the lane: inside the sequence
     const int64_t qrow = start + min(qi, len - 1);
 
-    bf16x8 qf[KS];
+    Core core;
+    core.init(lane);
 #pragma unroll
     for (int s = 0; s < KS; s++)
-        qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(a.q + qrow * a.ldq + head * a.q_head + 16 * s + 8 * hf));
+        core.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(a.q + qrow * a.ldq + head * a.q_head + 16 * s + 8 * hf));
 
-    const int keys = min(len, (tile + 1) * PA_ROWS), n_tiles = (keys + PA_KEYS - 1) / PA_KEYS;
-    auto k_swizzle = [](int r) __attribute__((always_inline)) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
-    auto v_swizzle = [](int r) __attribute__((always_inline)) { return HD == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
+    const int n_tiles = (min(len, (tile + 1) * PA_ROWS) + CORE_KEYS - 1) / CORE_KEYS;
+    // the wave's own: tiles that all of its queries see whole, and all it has anything to do with
+    const int n_mine = q0 < len ? min(n_tiles, (min(q0 + 31, len - 1) + CORE_KEYS) / CORE_KEYS) : 0, n_whole = min((q0 + 1) / CORE_KEYS, n_mine);
     const uint16_t *kbase = a.k + (int64_t)start * a.ldk + kvh * a.k_head, *vbase = a.v + (int64_t)start * a.ldv + kvh * a.v_head;
-    auto fetch = [&](int t, int buf) __attribute__((always_inline)) {
+    const uint32_t lds = (uint32_t)(size_t)((__attribute__((address_space(3))) unsigned char *)smem);
+    // The wave's part of a tile is rows wave * 64 / PA_WAVES .., RPI of them an instruction: a descriptor at the tile's first row, this lane's row and column
+    // in a register (one for each instruction: the swizzle's share of the instruction's row).
+    constexpr int R0 = CORE_KEYS / PA_WAVES;
+    const int lr = lane / GPR, lp = lane % GPR;
+    auto place = [&](int i, int r, int64_t ld, bool is_v) __attribute__((always_inline)) {
+        const int rs = R0 * wave + RPI * i + lr;                                        // the tile's row, of which row r is read
+        return (uint32_t)(r * (int)ld * 2 + (lp ^ (is_v ? Core::v_swizzle(rs) : Core::k_swizzle(rs))) * 16);
+    };
+    uint32_t k_off[LOADS], v_off[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) {
+        k_off[i] = place(i, R0 * wave + RPI * i + lr, a.ldk, false);
+        v_off[i] = place(i, R0 * wave + RPI * i + lr, a.ldv, true);
+    }
+    auto fetch = [&](int t, bool is_v) __attribute__((always_inline)) {
+        unsigned char *dst = smem + (is_v ? 2 * TILE : 0) + (t & 1) * TILE + wave * (TILE / PA_WAVES);
+        const int64_t ld = is_v ? a.ldv : a.ldk;
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)((is_v ? vbase : kbase) + (int64_t)t * CORE_KEYS * ld), 0, 0xFFFFFFFF, 0x00027000);
+        const int rows = len - t * CORE_KEYS;
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
-            const int piece = wave * LOADS + i, r = piece * RPI + lane / GPR, p = lane % GPR;
-            const int64_t key = min(t * PA_KEYS + r, len - 1);
-            const uint16_t *ks = kbase + key * a.ldk + (p ^ k_swizzle(r)) * 8, *vs = vbase + key * a.ldv + (p ^ v_swizzle(r)) * 8;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)ks,
-                                             (__attribute__((address_space(3))) void *)(smem + buf * 2 * TILE + piece * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)vs,
-                                             (__attribute__((address_space(3))) void *)(smem + buf * 2 * TILE + TILE + piece * 1024), 16, 0, 0);
+            uint32_t off = is_v ? v_off[i] : k_off[i];
+            if (rows < CORE_KEYS) off = place(i, min(R0 * wave + RPI * i + lr, rows - 1), ld, is_v);   // (behind the end: the last row again, which nobody sees)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(dst + i * 1024), 16, off, 0, 0, 0);
         }
     };
-
-    f32x16 o[NT];
-#pragma unroll
-    for (int n = 0; n < NT; n++) o[n] = f32x16{};
-    float m_run = -INFINITY, l_run = 0.f;
-
-    fetch(0, 0);
-    for (int t = 0; t < n_tiles; t++) {
-        __builtin_amdgcn_s_waitcnt(0x0F70);                                             // vmcnt(0): this wave's part of the tile is in LDS
-        __syncthreads();                                                                // everyone's is, and everyone has read the other buffer
-        if (t + 1 < n_tiles) fetch(t + 1, (t + 1) & 1);
-        const int key0 = t * PA_KEYS;
-        if (key0 > q0 + 31 || q0 >= len) continue;                                      // nothing here for this wave's queries
-        const unsigned char *kt = smem + (t & 1) * 2 * TILE, *vt = kt + TILE;
-        f32x16 s[2];
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            s[h] = f32x16{};
-#pragma unroll
-            for (int ks = 0; ks < KS; ks++) {
-                const int r = 32 * h + c;
-                const bf16x8 kf = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(kt + r * (HD * 2) + (((2 * ks + hf) ^ k_swizzle(r)) * 16)));
-                s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ks], s[h], 0, 0, 0);
-            }
-        }
-        const bool need_mask = key0 + PA_KEYS - 1 > q0;
-        if (need_mask) {
-#pragma unroll
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int e = 0; e < 16; e++) s[h][e] = key0 + 32 * h + 8 * (e >> 2) + 4 * hf + (e & 3) <= qi ? s[h][e] : -INFINITY;
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 16; e++) mx = fmaxf(mx, fmaxf(s[0][e], s[1][e]));
-        if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
-            const float m_new = fmaxf(m_run, fmaxf(mx, pa_other_half(mx)));
-            const float alpha = m_new == -INFINITY ? 1.f : pa_exp2((m_run - m_new) * a.scale_log2);
-            m_run = m_new;
-            l_run *= alpha;
-#pragma unroll
-            for (int n = 0; n < NT; n++) o[n] *= alpha;
-        }
-        const float base = m_run == -INFINITY ? 0.f : m_run * a.scale_log2;
-        float ps = 0.f;
+    auto landed = [&]() __attribute__((always_inline)) {                                // everyone's loads are in LDS, everyone's reads are done
+        __builtin_amdgcn_s_waitcnt(0x0070);                                             // vmcnt(0), lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    auto k_tile = [&](int t) __attribute__((always_inline)) { return lds + (t & 1) * TILE; };
+    auto v_tile = [&](int t) __attribute__((always_inline)) { return lds + 2 * TILE + (t & 1) * TILE; };
+    auto mask = [&](int t, f32x16 (&s)[2]) __attribute__((always_inline)) {
+        int last = qi - t * CORE_KEYS - 4 * hf;                                         // of the keys 8 i + r that this lane holds
+        asm volatile("" : "+v"(last));
 #pragma unroll
         for (int h = 0; h < 2; h++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                s[h][e] = pa_exp2(__builtin_fmaf(s[h][e], a.scale_log2, -base));
-                ps += s[h][e];
-            }
-        l_run += ps;
-#pragma unroll
-        for (int kk = 0; kk < PA_KEYS / 16; kk++) {
-            const int h = kk >> 1, e0 = 8 * (kk & 1);
-            uint32_t pk[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++) pk[e] = pa_pk_bf16(s[h][e0 + 2 * e], s[h][e0 + 2 * e + 1]);
-            const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
-#pragma unroll
-            for (int n = 0; n < NT; n++) {
-                typedef __attribute__((ext_vector_type(4))) short s4;
-                typedef __attribute__((ext_vector_type(8))) short s8;
-                typedef __attribute__((address_space(3))) s4 *lds_s4;
-                s4 half[2];
-#pragma unroll
-                for (int x = 0; x < 2; x++) {
-                    // four keys of 16 columns a group of 16 lanes: this lane names one key's four columns and gets its own column of the four keys
-                    const int r = 16 * kk + 8 * x + 4 * hf + ((c & 15) >> 2), col = 32 * n + (c & 16) + 4 * (c & 3);
-                    half[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(vt + r * (HD * 2) + (((col >> 3) ^ v_swizzle(r)) * 16) + (col & 4) * 2));
-                }
-                bf16x8 vf = __builtin_bit_cast(bf16x8, s8{half[0][0], half[0][1], half[0][2], half[0][3], half[1][0], half[1][1], half[1][2], half[1][3]});
-                if (need_mask && __builtin_amdgcn_ballot_w64(has_nonfinite(vf)) != 0) {
-                    bf16x8 up, down;
-                    split_nonfinite(vf, up, down);
-                    uint32_t one[4];
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const int key = key0 + 16 * kk + 8 * (e >> 1) + 4 * hf + 2 * (e & 1);
-                        one[e] = (key <= qi ? 0x3F80u : 0u) | (key + 1 <= qi ? 0x3F800000u : 0u);
-                    }
-                    const bf16x8 seen = __builtin_bit_cast(bf16x8, make_uint4(one[0], one[1], one[2], one[3]));
-                    const f32x16 a_up = __builtin_amdgcn_mfma_f32_32x32x16_bf16(up, seen, f32x16{}, 0, 0, 0);
-                    const f32x16 a_down = __builtin_amdgcn_mfma_f32_32x32x16_bf16(down, seen, f32x16{}, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 16; e++) o[n][e] += nonfinite_term(a_up[e], a_down[e]);
-                }
-                o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[n], 0, 0, 0);
-            }
-        }
+            for (int e = 0; e < 16; e++) s[h][e] = 32 * h + 8 * (e >> 2) + (e & 3) <= last ? s[h][e] : -INFINITY;
+    };
+
+    // Scores run a tile ahead: while a tile's scores become probabilities, the matrix cores work on the next one's.  So K is fetched two tiles ahead, V one.
+    f32x16 s[2];
+    uint32_t p[16], odd = 0;
+    int t = 0;
+    fetch(0, false);
+    fetch(0, true);
+    for (; t < n_whole; t++) {
+        landed();
+        if (t + 1 < n_tiles) { fetch(t + 1, false); fetch(t + 1, true); }
+        core.scores(k_tile(t), s);
+        core.probabilities(s, a.scale_log2, p, t == 0);
+        core.template add_values<false>(v_tile(t), p, odd);
     }
+    for (; t < n_tiles; t++) {
+        landed();
+        if (t + 1 < n_tiles) { fetch(t + 1, false); fetch(t + 1, true); }
+        if (t >= n_mine) continue;
+        core.scores(k_tile(t), s);
+        mask(t, s);
+        core.probabilities(s, a.scale_log2, p, true);
+        core.template add_values<true>(v_tile(t), p, odd);
+    }
+    const int n_plain = n_whole;
+    if (__builtin_amdgcn_ballot_w64(odd != 0) != 0)
+        for (t = n_plain; t < n_mine; t++) {
+            const int past = qi - t * CORE_KEYS;                                        // keys 0 .. past of the tile are seen
+            core.add_nonfinite(vbase + (int64_t)t * CORE_KEYS * a.ldv, a.ldv, len - 1 - t * CORE_KEYS, past >= 63 ? ~0ull : (2ull << past) - 1);
+        }
     if (qi >= len) return;
-    const float l = l_run + pa_other_half(l_run), inv = 1.0f / l;
+    const float inv = 1.0f / core_sum_halves(core.l_run);
     uint16_t *dst = a.out + qrow * a.ldo + (int64_t)head * HD + 4 * hf;
 #pragma unroll
     for (int n = 0; n < NT; n++)
 #pragma unroll
         for (int i = 0; i < 4; i++)
-            *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) = make_uint2(pa_pk_bf16(o[n][4 * i] * inv, o[n][4 * i + 1] * inv),
-                                                                          pa_pk_bf16(o[n][4 * i + 2] * inv, o[n][4 * i + 3] * inv));
+            *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) = make_uint2(core_pk_bf16(core.o[n][4 * i] * inv, core.o[n][4 * i + 1] * inv),
+                                                                          core_pk_bf16(core.o[n][4 * i + 2] * inv, core.o[n][4 * i + 3] * inv));
 }
 
 extern "C" int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_head_stride, const void *d_k, int64_t ldk, int64_t k_head_stride,
@@ -223,6 +180,7 @@ extern "C" int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_hea
     if ((ldq | ldk | ldv | q_head_stride | k_head_stride | v_head_stride | ldo) & 7 ||
         ((uintptr_t)d_q | (uintptr_t)d_k | (uintptr_t)d_v | (uintptr_t)d_out) & 15)
         return bita_set_error(BITA_ERR_UNSUPPORTED, "%s: strides must be multiples of 8 elements, pointers of 16 bytes", who);
+    if (ldk > PA_MAX_LD || ldv > PA_MAX_LD) return bita_set_error(BITA_ERR_UNSUPPORTED, "%s: rows of k and v at most %d elements apart", who, PA_MAX_LD);
     const int64_t tiles = (int64_t)n_tokens / PA_ROWS + n_seqs, wgs = tiles * n_heads;          // no tiling of the sequences has more
     if (wgs > (int64_t)((1ull << 32) / (PA_WAVES * 64)) - 1)
         return bita_set_error(BITA_ERR_UNSUPPORTED, "%s: %lld workgroups", who, (long long)wgs);
@@ -230,8 +188,8 @@ extern "C" int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_hea
     const PromptArgs a = {(const uint16_t *)d_q, (const uint16_t *)d_k, (const uint16_t *)d_v, ldq, q_head_stride, ldk, k_head_stride, ldv, v_head_stride, ldo,
                           d_cu_seqlens, n_seqs, n_tokens, n_heads, n_heads / n_kv_heads, 1.4426950408889634f / sqrtf((float)head_dim), (uint16_t *)d_out};
     hipStream_t s = (hipStream_t)stream;
-    if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_kernel<128>), dim3((unsigned)wgs), dim3(PA_WAVES * 64), 4 * PA_KEYS * 128 * 2, s, a);
-    else hipLaunchKernelGGL((prompt_attn_kernel<64>), dim3((unsigned)wgs), dim3(PA_WAVES * 64), 4 * PA_KEYS * 64 * 2, s, a);
+    if (head_dim == 128) hipLaunchKernelGGL((prompt_attn_kernel<128>), dim3((unsigned)wgs), dim3(PA_WAVES * 64), 4 * AttnCore<128>::TILE, s, a);
+    else hipLaunchKernelGGL((prompt_attn_kernel<64>), dim3((unsigned)wgs), dim3(PA_WAVES * 64), 4 * AttnCore<64>::TILE, s, a);
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;
 }
