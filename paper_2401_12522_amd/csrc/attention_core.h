@@ -154,6 +154,41 @@ struct AttnCore {
         }
         l_run += sum;
     }
+    // The next tile's scores while this one's become probabilities: the matrix instructions of the first between the vector instructions of the
+    // second, pair by pair.
+    __device__ __forceinline__ void scores_and_probabilities(uint32_t tile, f32x16 (&next)[2], f32x16 (&s)[2], float scale_log2, uint32_t (&p)[16]) {
+        constexpr int GROUPS = 2 * KS / 4, PAIRS = 16 / (2 * KS);               // pairs of probabilities behind each matrix instruction
+        const uint32_t at = tile + k_at;
+        KFrag k[2];
+        float sum[2] = {0.f, 0.f};
+        k_read<0>(at, k[0]);
+        core_for<0, GROUPS>([&](auto g_) __attribute__((always_inline)) {
+            constexpr int g = decltype(g_)::value, h = 4 * g / KS;
+            if constexpr (g + 1 < GROUPS) k_read<g + 1>(at, k[(g + 1) & 1]);
+            k_wait<(g + 1 < GROUPS) ? 4 : 0>(k[g & 1]);
+            if constexpr (4 * g % KS == 0) next[h] = f32x16{};
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                next[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[g & 1].f[i]), q[(4 * g + i) % KS], next[h], 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < PAIRS; j++) {
+                    const int e = 2 * ((4 * g + i) * PAIRS + j);
+                    const float x = core_exp2(__builtin_fmaf(s[e >> 4][e & 15], scale_log2, -base)), y = core_exp2(__builtin_fmaf(s[e >> 4][(e & 15) + 1], scale_log2, -base));
+                    sum[0] += x;
+                    sum[1] += y;
+                    p[e >> 1] = core_pk_bf16(x, y);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+        float total = sum[0] + sum[1];
+        if (__builtin_amdgcn_ballot_w64(total > 0x1p60f || l_run + total == 0.f) != 0) {
+            asm volatile("" : "+v"(s[0]), "+v"(s[1]));                          // (else the maximum is taken of every tile, ahead of time)
+            take_maximum(largest(s), scale_log2);
+            total = exponentials(s, scale_log2, p);
+        }
+        l_run += total;
+    }
     // V fragments of 16 keys: column tile n of the head
     struct VFrag { s16x4_t half[NT][2]; };
     template <int KK>

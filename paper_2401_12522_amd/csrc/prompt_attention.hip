@@ -82,35 +82,25 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void prompt_attn_kernel(PromptArg
         core.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(a.q + qrow * a.ldq + head * a.q_head + 16 * s + 8 * hf));
 
     const int n_tiles = (min(len, (tile + 1) * PA_ROWS) + CORE_KEYS - 1) / CORE_KEYS;
-    // the wave's own: tiles that all of its queries see whole, and all it has anything to do with
-    const int n_mine = q0 < len ? min(n_tiles, (min(q0 + 31, len - 1) + CORE_KEYS) / CORE_KEYS) : 0, n_whole = min((q0 + 1) / CORE_KEYS, n_mine);
+    const int n_whole = q0 / CORE_KEYS;                                                 // tiles that all of the wave's queries see whole
     const uint16_t *kbase = a.k + (int64_t)start * a.ldk + kvh * a.k_head, *vbase = a.v + (int64_t)start * a.ldv + kvh * a.v_head;
     const uint32_t lds = (uint32_t)(size_t)((__attribute__((address_space(3))) unsigned char *)smem);
-    // The wave's part of a tile is rows wave * 64 / PA_WAVES .., RPI of them an instruction: a descriptor at the tile's first row, this lane's row and column
-    // in a register (one for each instruction: the swizzle's share of the instruction's row).
-    constexpr int R0 = CORE_KEYS / PA_WAVES;
+    // The wave's part of a tile is rows wave * 64 / PA_WAVES .., RPI of them an instruction: a descriptor at the tile's first row (what lies behind the
+    // sequence's last one is out of its range, and 0), the instruction's row in the scalar offset, this lane's row and column in two
+    // registers; the swizzle's share of the instruction's row is an exclusive or.
+    constexpr int R0 = CORE_KEYS / PA_WAVES, K_STEP = 4, V_STEP = HD == 128 ? 1 : 2;
     const int lr = lane / GPR, lp = lane % GPR;
-    auto place = [&](int i, int r, int64_t ld, bool is_v) __attribute__((always_inline)) {
-        const int rs = R0 * wave + RPI * i + lr;                                        // the tile's row, of which row r is read
-        return (uint32_t)(r * (int)ld * 2 + (lp ^ (is_v ? Core::v_swizzle(rs) : Core::k_swizzle(rs))) * 16);
-    };
-    uint32_t k_off[LOADS], v_off[LOADS];
-#pragma unroll
-    for (int i = 0; i < LOADS; i++) {
-        k_off[i] = place(i, R0 * wave + RPI * i + lr, a.ldk, false);
-        v_off[i] = place(i, R0 * wave + RPI * i + lr, a.ldv, true);
-    }
+    const uint32_t k_row = lr * (uint32_t)a.ldk * 2, k_col = (lp ^ Core::k_swizzle(lr)) * 16;
+    const uint32_t v_row = lr * (uint32_t)a.ldv * 2, v_col = (lp ^ Core::v_swizzle(lr)) * 16;
     auto fetch = [&](int t, bool is_v) __attribute__((always_inline)) {
         unsigned char *dst = smem + (is_v ? 2 * TILE : 0) + (t & 1) * TILE + wave * (TILE / PA_WAVES);
-        const int64_t ld = is_v ? a.ldv : a.ldk;
-        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)((is_v ? vbase : kbase) + (int64_t)t * CORE_KEYS * ld), 0, 0xFFFFFFFF, 0x00027000);
-        const int rows = len - t * CORE_KEYS;
+        const uint32_t ld = 2 * (uint32_t)(is_v ? a.ldv : a.ldk), rows = min(len - t * CORE_KEYS, CORE_KEYS);
+        const __amdgpu_buffer_rsrc_t rsrc =
+            __builtin_amdgcn_make_buffer_rsrc((void *)((is_v ? vbase : kbase) + (int64_t)t * CORE_KEYS * (is_v ? a.ldv : a.ldk)), 0, (rows - 1) * ld + HD * 2, 0x00027000);
 #pragma unroll
-        for (int i = 0; i < LOADS; i++) {
-            uint32_t off = is_v ? v_off[i] : k_off[i];
-            if (rows < CORE_KEYS) off = place(i, min(R0 * wave + RPI * i + lr, rows - 1), ld, is_v);   // (behind the end: the last row again, which nobody sees)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(dst + i * 1024), 16, off, 0, 0, 0);
-        }
+        for (int i = 0; i < LOADS; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(dst + i * 1024), 16,
+                                                     is_v ? (v_col ^ (16 * V_STEP * i)) + v_row : (k_col ^ (16 * K_STEP * i)) + k_row, (R0 * wave + RPI * i) * ld, 0, 0);
     };
     auto landed = [&]() __attribute__((always_inline)) {                                // everyone's loads are in LDS, everyone's reads are done
         __builtin_amdgcn_s_waitcnt(0x0070);                                             // vmcnt(0), lgkmcnt(0)
@@ -129,34 +119,44 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void prompt_attn_kernel(PromptArg
             for (int e = 0; e < 16; e++) s[h][e] = 32 * h + 8 * (e >> 2) + (e & 3) <= last ? s[h][e] : -INFINITY;
     };
 
-    // Scores run a tile ahead: while a tile's scores become probabilities, the matrix cores work on the next one's.  So K is fetched two tiles ahead, V one.
+    auto turn = [&](int t) __attribute__((always_inline)) {                             // tile t's V and t + 1's K are there; the next are asked for
+        landed();
+        if (t + 2 < n_tiles) fetch(t + 2, false);
+        if (t + 1 < n_tiles) fetch(t + 1, true);
+    };
+
+    // Scores run a tile ahead: while a tile's become probabilities, the matrix cores work on the next one's.  So K is fetched two tiles
+    // ahead, V one.  A wave's queries lie in one tile of keys: those before it are seen whole, behind it there is only the others' pace to keep.
     f32x16 s[2];
     uint32_t p[16], odd = 0;
     int t = 0;
     fetch(0, false);
+    landed();
     fetch(0, true);
-    for (; t < n_whole; t++) {
-        landed();
-        if (t + 1 < n_tiles) { fetch(t + 1, false); fetch(t + 1, true); }
-        core.scores(k_tile(t), s);
-        core.probabilities(s, a.scale_log2, p, t == 0);
-        core.template add_values<false>(v_tile(t), p, odd);
-    }
-    for (; t < n_tiles; t++) {
-        landed();
-        if (t + 1 < n_tiles) { fetch(t + 1, false); fetch(t + 1, true); }
-        if (t >= n_mine) continue;
-        core.scores(k_tile(t), s);
+    if (n_tiles > 1) fetch(1, false);
+    if (q0 < len) {
+        core.scores(k_tile(0), s);
+        if (n_whole == 0) mask(0, s);
+        core.take_maximum(core.largest(s), a.scale_log2);                               // (what every query's reference starts with)
+        for (; t < n_whole; t++) {
+            turn(t);
+            f32x16 next[2];
+            core.scores_and_probabilities(k_tile(t + 1), next, s, a.scale_log2, p);
+            core.template add_values<false>(v_tile(t), p, odd);
+            s[0] = next[0];
+            s[1] = next[1];
+        }
+        turn(t);
         mask(t, s);
         core.probabilities(s, a.scale_log2, p, true);
         core.template add_values<true>(v_tile(t), p, odd);
-    }
-    const int n_plain = n_whole;
-    if (__builtin_amdgcn_ballot_w64(odd != 0) != 0)
-        for (t = n_plain; t < n_mine; t++) {
+        if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
             const int past = qi - t * CORE_KEYS;                                        // keys 0 .. past of the tile are seen
             core.add_nonfinite(vbase + (int64_t)t * CORE_KEYS * a.ldv, a.ldv, len - 1 - t * CORE_KEYS, past >= 63 ? ~0ull : (2ull << past) - 1);
         }
+        t++;
+    }
+    for (; t < n_tiles; t++) turn(t);
     if (qi >= len) return;
     const float inv = 1.0f / core_sum_halves(core.l_run);
     uint16_t *dst = a.out + qrow * a.ldo + (int64_t)head * HD + 4 * hf;
