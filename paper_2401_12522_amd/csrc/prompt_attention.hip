@@ -26,8 +26,8 @@ struct PromptArgs {
     uint16_t *out;
 };
 
-// The tile's sequence, its first token and length, and the tile's number inside it, from the sequences' ends: tiles are counted over
-// the sequences, 64 of them a step.  false: no such tile.
+// The workgroup's tile of queries: its sequence's first token and length, and its number in the sequence.  Tiles count from the longest walk
+// down, over 64 sequences (a lane each) at a time: of every number the tiles that sequences have, until `tile` is reached.  false: no such tile.
 __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &start, int &len, int &mine) {
     const int lane = threadIdx.x & 63;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
@@ -38,21 +38,32 @@ __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &star
             n = min(max(a.cu[b + 1], s), a.n_tokens) - s;
         }
         const int tiles = (n + PA_ROWS - 1) / PA_ROWS;
-        int upto = tiles;
+        int all = tiles, most = tiles;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const int other = __shfl_up(upto, d);
-            if (lane >= d) upto += other;
+            all += __shfl_xor(all, d);
+            most = max(most, __shfl_xor(most, d));
         }
-        const int all = __shfl(upto, 63);
-        if (tile < all) {
-            const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > tile));
+        all = __builtin_amdgcn_readfirstlane(all);
+        if (tile >= all) {
+            tile -= all;
+            continue;
+        }
+        for (int k = __builtin_amdgcn_readfirstlane(most) - 1;; k--) {                  // (ends: `all` is the sum of these counts over k)
+            const uint64_t has = __builtin_amdgcn_ballot_w64(tiles > k);
+            const int count = __popcll(has);
+            if (tile >= count) {
+                tile -= count;
+                continue;
+            }
+            // the lane that has `tile` others before it
+            const bool me = tiles > k && __popcll(has & ((1ull << lane) - 1)) == tile;
+            const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(me));
             start = __builtin_amdgcn_readlane(s, at);
             len = __builtin_amdgcn_readlane(n, at);
-            mine = tile - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at));
+            mine = k;
             return true;
         }
-        tile -= all;
     }
     return false;
 }
@@ -68,10 +79,7 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void prompt_attn_kernel(PromptArg
     const int j = blockIdx.x % a.Hq;
     const int head = a.Hq % 8 == 0 ? (j & 7) * (a.Hq >> 3) + (j >> 3) : j;              // an XCD (ids go round) takes neighbouring heads
     int start, len, tile;
-    if (!pa_find(a, blockIdx.x / a.Hq, start, len, tile)) return;
-    start = __builtin_amdgcn_readfirstlane(start);                                      // (the same in all lanes, which the compiler cannot know)
-    len = __builtin_amdgcn_readfirstlane(len);
-    tile = (len + PA_ROWS - 1) / PA_ROWS - 1 - __builtin_amdgcn_readfirstlane(tile);    // the longest walk first
+    if (!pa_find(a, blockIdx.x / a.Hq, start, len, tile)) return;                       // (the same in all lanes, and the compiler knows)
     const int q0 = tile * PA_ROWS + wave * 32, qi = q0 + c, kvh = head / a.qpk;         // of the wave, of the lane: inside the sequence
     const int64_t qrow = start + min(qi, len - 1);
 
