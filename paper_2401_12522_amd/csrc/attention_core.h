@@ -118,12 +118,15 @@ struct AttnCore {
     __device__ __forceinline__ void take_maximum(float mx, float scale_log2) {
         if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
             const float m_new = fmaxf(m_run, core_max_halves(mx));
-            const float alpha = m_new == -INFINITY ? 1.f : core_exp2((m_run - m_new) * scale_log2);
+            // in two halves: what is rescaled may be up to 2^60 (probabilities), and one factor below 2^-126 would be 0
+            const float alpha = m_new == -INFINITY ? 1.f : core_exp2((m_run - m_new) * (0.5f * scale_log2));
             m_run = m_new;
             base = m_new == -INFINITY ? 0.f : m_new * scale_log2;
-            l_run *= alpha;
+            l_run = l_run * alpha * alpha;
 #pragma unroll
-            for (int n = 0; n < NT; n++) o[n] *= alpha;
+            for (int n = 0; n < NT; n++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) o[n][e] = o[n][e] * alpha * alpha;
         }
     }
     // scores to probabilities 2^(score scale - base) as bf16 pairs, in the order of the registers; their sum

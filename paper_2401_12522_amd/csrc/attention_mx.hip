@@ -12,9 +12,9 @@
 //    B operand of O^T = V^T P^T if that product takes the keys in the same order: probabilities stay in registers.
 //  * V^T needs eight keys of one column in a lane: V goes to LDS as bf16 rows and comes back by transposed reads.  The region is the wave's own,
 //    and its LDS instructions run in order, so there is no barrier in the loop.
-#include "mx.h"
-#include "nonfinite.h"
 #include <cmath>
+#include "mx.h"
+#include "attention_core.h"
 
 #define AMX_CHUNK 32
 #define AMX_WAVES 4
@@ -40,10 +40,70 @@ struct AmxArgs {
     const uint16_t *q, *k_rows, *v_rows, *prompt_k, *prompt_v;
     MxRows k_at, v_at;
     const int32_t *ctx_len, *token;
-    int P, R, qpk, ctx_hint, n_tiles, n_splits;                 // tiles of 16 U queries
+    int P, R, qpk, ctx_hint, n_tiles, n_splits, per_split;      // tiles of a workgroup's queries, shares of the keys, chunks (tiles) of a share
     float scale_log2;
     float *part_o, *part_ml;
     uint16_t *out;
+};
+
+// Workgroup id -> (tile of queries, share of the keys, sequence, K/V head).  The tiles that read the same keys go to one XCD, one behind the other: ids go round
+// over the 8 XCDs, and the shares with them, a head's neighbours first.  (Quotients are worked out in vector registers: without being told, the compiler
+// keeps what follows from them there, descriptors too.)
+__device__ __forceinline__ bool amx_place(const AmxArgs &a, int &tile, int &split, int &b, int &h) {
+    const int n_groups = a.kv.batch * a.kv.Hkv, i = blockIdx.x >> 3;
+    const int set = __builtin_amdgcn_readfirstlane(i / a.n_tiles), unit = (blockIdx.x & 7) + 8 * set;
+    tile = i - set * a.n_tiles;
+    split = __builtin_amdgcn_readfirstlane(unit / n_groups);
+    const int group = unit - split * n_groups;
+    b = __builtin_amdgcn_readfirstlane(group / a.kv.Hkv);
+    h = group - b * a.kv.Hkv;
+    return split < a.n_splits;
+}
+
+// Sixteen neighbouring keys' codes and scale bytes, from one page or the contiguous cache: lane (g, c) = (l / 16, l % 16) takes a quarter of key c,
+// HD / 4 values.  The keys' first row is known to the whole wave, so a descriptor holds it, with the keys that there are (none: what
+// is loaded is 0, which decodes to 0), and a lane's own offsets never change.
+template <int HD, int BITS>
+struct MxKeys {
+    static constexpr int DW = HD / 4 * BITS / 32, ROW = HD * BITS / 8, SROW = HD / 32;      // dwords of a lane, bytes of a row's codes, and of its scales
+    static constexpr int PARTS = HD / 32;                                                   // eights of values of a lane
+    uint32_t d[DW], scale;
+
+    static __device__ __forceinline__ uint32_t code_offset(int lane) { return (lane & 15) * ROW + (lane >> 4) * (DW * 4); }
+    static __device__ __forceinline__ uint32_t scale_offset(int lane) { return (lane & 15) * SROW + (HD == 128 ? lane >> 4 : lane >> 5); }
+    // the page of keys key0 .. key0 + 15 of sequence b, of which there are `length` (a number the whole wave has)
+    static __device__ __forceinline__ int page_of(const KvMx &kv, int b, int key0, int length) {
+        if (!kv.table) return b;
+        const int32_t *at = kv.table + (int64_t)b * kv.max_pages + (min(key0, length - 1) >> kv.page_lg);
+        return __builtin_amdgcn_readfirstlane(min(max(*(const __attribute__((address_space(4))) int32_t *)(uintptr_t)at, 0), kv.n_pages - 1));      // (through the scalar cache)
+    }
+    __device__ __forceinline__ void load(const KvMx &kv, const unsigned char *codes, const uint8_t *scales, int h, int key0, int length, int page,
+                                         uint32_t code_off, uint32_t scale_off) {
+        const int64_t row = ((int64_t)page * kv.Hkv + h) * kv.page_rows + (key0 & kv.slot_mask);
+        const int n = __builtin_amdgcn_readfirstlane(min(max(length - key0, 0), 16));       // (limits are taken in vector registers, and the descriptor with them)
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void *)(codes + row * ROW), 0, n * ROW, 0x00027000);
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)(scales + row * SROW), 0, n * SROW, 0x00027000);
+        if constexpr (DW == 2) {
+            typedef __attribute__((ext_vector_type(2))) uint32_t u2;
+            const u2 v = __builtin_amdgcn_raw_buffer_load_b64(rc, code_off, 0, 0);
+            d[0] = v[0]; d[1] = v[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < DW; i += 4) {
+                const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(rc, code_off + 4 * i, 0, 0);
+                d[i] = v[0]; d[i + 1] = v[1]; d[i + 2] = v[2]; d[i + 3] = v[3];
+            }
+        }
+        scale = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rs, scale_off, 0, 0);
+    }
+    __device__ __forceinline__ void decode(bf16x8 (&x)[PARTS]) const {
+        const float s = mx_scale(scale);
+#pragma unroll
+        for (int i = 0; i < PARTS; i++) {
+            if constexpr (BITS == 4) x[i] = mx_decode4(d[i], s);
+            else x[i] = mx_decode8(d[2 * i], d[2 * i + 1], s);
+        }
+    }
 };
 
 template <int HD, int U>
@@ -55,29 +115,18 @@ struct AmxCfg {
     static constexpr int SMEM = ML + 2 * U * AMX_WAVES * 16 * 4;
 };
 
-// one chunk's codes and scale bytes in registers: of keys c and 16 + c
-template <int HD, int BITS>
-struct AmxRaw {
-    static constexpr int DW = HD / 4 * BITS / 32;                       // dwords of a lane's part of a key: 4 or 8 (128), 2 or 4 (64)
-    uint32_t k[2][DW], v[2][DW];
-    uint32_t ks[2], vs[2];
-};
-
 template <int HD, int BITS, int U>
 __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
     using C = AmxCfg<HD, U>;
-    using Raw = AmxRaw<HD, BITS>;
-    constexpr int KS = C::KS, NT = C::NT, VPL = C::VPL, DW = Raw::DW, W = AMX_WAVES;
+    using Keys = MxKeys<HD, BITS>;
+    constexpr int KS = C::KS, NT = C::NT, VPL = C::VPL, W = AMX_WAVES;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // The tiles that read the same keys (a share of a K/V head's) go to one XCD, one behind the other: ids go round over the 8 XCDs, and
-    // the shares with them, a head's neighbours first.
-    const int Hkv = a.kv.Hkv, n_groups = a.kv.batch * Hkv, i_xcd = blockIdx.x >> 3;
-    const int unit = (blockIdx.x & 7) + 8 * (i_xcd / a.n_tiles), tile = i_xcd % a.n_tiles, split = unit / n_groups, group = unit - split * n_groups;
-    if (split >= a.n_splits) return;
-    const int b = group / Hkv, h = group - b * Hkv;
-    const int Lc = min(max(a.ctx_len[b], 0), min(a.ctx_hint, a.kv.smax));
+    const int Hkv = a.kv.Hkv;
+    int tile, split, b, h;
+    if (!amx_place(a, tile, split, b, h)) return;
+    const int Lc = __builtin_amdgcn_readfirstlane(min(max(a.ctx_len[b], 0), min(a.ctx_hint, a.kv.smax)));
     const int nq = a.R * a.qpk;
 
     // queries: lane (g, c) holds, of query c of every tile, values VPL g + 8 s .. +8 of k-step s
@@ -93,8 +142,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
     const int last_row = min((tile + 1) * U * 16 - 1, nq - 1) / a.qpk;          // of the workgroup: pass rows behind it are nobody's ancestors
 
     const int n_p = (a.P + AMX_CHUNK - 1) / AMX_CHUNK, n_c = (Lc + AMX_CHUNK - 1) / AMX_CHUNK, n_r = last_row / AMX_CHUNK + 1;
-    const int n_chunks = n_p + n_c + n_r, per_split = (n_chunks + a.n_splits - 1) / a.n_splits;
-    const int first = split * per_split + wave, end = min(n_chunks, (split + 1) * per_split);
+    const int first = split * a.per_split + wave, end = min(n_c + n_p + n_r, (split + 1) * a.per_split);
 
     f32x4 o[U][NT];
     float m_run[U], base[U], l_run[U];
@@ -108,38 +156,6 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
     unsigned char *v_lds = smem + wave * C::V_BYTES;
     // V row rho in LDS: 16-byte column p of it at position p ^ swizzle(rho)
     auto v_swizzle = [](int rho) __attribute__((always_inline)) { return HD == 128 ? 2 * (rho & 7) : 2 * ((rho >> 1) & 3); };
-
-    auto load = [&](int chunk, Raw &r) __attribute__((always_inline)) {
-        const int base_key = chunk * AMX_CHUNK;
-#pragma unroll
-        for (int tt = 0; tt < 2; tt++) {
-            const int key = min(base_key + 16 * tt + c, Lc - 1);                // (behind the end: the last one once more, which has probability 0 there)
-            const int64_t at = mx_row(a.kv, b, h, key);
-            const int64_t byte = at * (HD * BITS / 8) + g * (DW * 4);
-            const int64_t sc = at * (HD / 32) + (HD == 128 ? g : g >> 1);
-#pragma unroll
-            for (int d = 0; d < DW; d += (DW >= 4 ? 4 : 2)) {
-                if constexpr (DW >= 4) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(a.kv.k + byte + 4 * d), y = *reinterpret_cast<const uint4 *>(a.kv.v + byte + 4 * d);
-                    r.k[tt][d] = x.x; r.k[tt][d + 1] = x.y; r.k[tt][d + 2] = x.z; r.k[tt][d + 3] = x.w;
-                    r.v[tt][d] = y.x; r.v[tt][d + 1] = y.y; r.v[tt][d + 2] = y.z; r.v[tt][d + 3] = y.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2 *>(a.kv.k + byte), y = *reinterpret_cast<const uint2 *>(a.kv.v + byte);
-                    r.k[tt][0] = x.x; r.k[tt][1] = x.y;
-                    r.v[tt][0] = y.x; r.v[tt][1] = y.y;
-                }
-            }
-            r.ks[tt] = a.kv.k_scale[sc];
-            r.vs[tt] = a.kv.v_scale[sc];
-        }
-    };
-    auto decode = [&](const uint32_t (&d)[DW], float scale, bf16x8 (&x)[KS]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int s = 0; s < KS; s++) {
-            if constexpr (BITS == 4) x[s] = mx_decode4(d[s], scale);
-            else x[s] = mx_decode8(d[2 * s], d[2 * s + 1], scale);
-        }
-    };
 
     // V rows rho = 16 tt + c as bf16 to LDS
     auto put_v = [&](int tt, const bf16x8 (&vf)[KS]) __attribute__((always_inline)) {
@@ -210,23 +226,40 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
     // ---- the cache
     int chunk = first;
     {
-        Raw raw;
+        // Two chunks' codes are on their way while a third is multiplied: a chunk's arithmetic is shorter than a trip to memory under load.  (One, where
+        // two tiles of queries make it longer and leave no registers.)
+        constexpr int DEPTH = U == 1 ? 2 : 1;
+        struct Chunk { Keys k[2], v[2]; int page[2]; };                         // of keys c and 16 + c; the pages to load from next
+        Chunk set[DEPTH];
+        const uint32_t code_off = Keys::code_offset(lane), scale_off = Keys::scale_offset(lane);
         const int stop = min(end, n_c);
-        if (chunk < stop) load(chunk, raw);
-        for (; chunk < stop; chunk += W) {
+        auto ask_pages = [&](Chunk &x, int chunk) __attribute__((always_inline)) {
+#pragma unroll
+            for (int tt = 0; tt < 2; tt++) x.page[tt] = Keys::page_of(a.kv, b, AMX_CHUNK * chunk + 16 * tt, Lc);
+        };
+        auto load = [&](Chunk &x, int chunk) __attribute__((always_inline)) {   // (behind the end: nothing is there, zeros come back)
+#pragma unroll
+            for (int tt = 0; tt < 2; tt++) {
+                x.k[tt].load(a.kv, a.kv.k, a.kv.k_scale, h, AMX_CHUNK * chunk + 16 * tt, Lc, x.page[tt], code_off, scale_off);
+                x.v[tt].load(a.kv, a.kv.v, a.kv.v_scale, h, AMX_CHUNK * chunk + 16 * tt, Lc, x.page[tt], code_off, scale_off);
+            }
+        };
+        auto step = [&](Chunk &x) __attribute__((always_inline)) {
             const int key0 = AMX_CHUNK * chunk;
             bf16x8 kf[2][KS];
 #pragma unroll
             for (int tt = 0; tt < 2; tt++) {
                 bf16x8 vf[KS];
-                decode(raw.k[tt], mx_scale(raw.ks[tt]), kf[tt]);
-                decode(raw.v[tt], mx_scale(raw.vs[tt]), vf);
+                x.k[tt].decode(kf[tt]);
+                x.v[tt].decode(vf);
                 put_v(tt, vf);
             }
-            if (chunk + W < stop) load(chunk + W, raw);
+            load(x, chunk + DEPTH * W);
+            ask_pages(x, chunk + 2 * DEPTH * W);
             f32x4 sc[U][2];
 #pragma unroll
             for (int u = 0; u < U; u++) scores(u, kf, sc[u]);
+            __builtin_amdgcn_sched_barrier(0);                                  // (K's registers are V's from here on)
             bf16x8 vt[NT];
             get_vt(vt);
             uint32_t bits = 0xFF;
@@ -240,6 +273,23 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
                 const bf16x8 pf = probabilities(u, sc[u], bits);
 #pragma unroll
                 for (int n = 0; n < NT; n++) o[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[n], pf, o[u][n], 0, 0, 0);
+            }
+            chunk += W;
+        };
+        if (chunk < stop) {
+#pragma unroll
+            for (int i = 0; i < DEPTH; i++) {
+                ask_pages(set[i], chunk + i * W);
+                load(set[i], chunk + i * W);
+                ask_pages(set[i], chunk + (i + DEPTH) * W);
+            }
+            while (true) {
+                step(set[0]);
+                if (chunk >= stop) break;
+                if constexpr (DEPTH > 1) {
+                    step(set[1]);
+                    if (chunk >= stop) break;
+                }
             }
         }
     }
@@ -349,7 +399,8 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
             }
             if (a.n_splits > 1) {
                 *reinterpret_cast<float4 *>(a.part_o + (qrow * a.n_splits + split) * HD + 16 * n + 4 * g) = x;
-                if (n == 0 && g == 0) *reinterpret_cast<float2 *>(a.part_ml + (qrow * a.n_splits + split) * 2) = make_float2(m_tot[u], absent ? 0.f : l_tot[u]);
+                if (n == 0 && g == 0)
+                    *reinterpret_cast<float2 *>(a.part_ml + (qrow * a.n_splits + split) * 2) = absent ? make_float2(-INFINITY, 0.f) : make_float2(m_tot[u], l_tot[u]);
                 continue;
             }
             // (a NaN sum stays one; a sum of nothing, or an absent row, gives zeros)
@@ -360,51 +411,320 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
     }
 }
 
-// o = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max m); a thread 4 values of a query's head
-template <int HD>
-__global__ __launch_bounds__(256) void attn_mx_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, int64_t n_queries, int n_splits,
-                                                            uint16_t *__restrict__ out) {
-    constexpr int LANES = HD / 4;
-    const int64_t qrow = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-    const int i = threadIdx.x % LANES * 4;
-    if (qrow >= n_queries) return;
-    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + qrow * n_splits;
-    float m = -INFINITY;
-    for (int s = 0; s < n_splits; s++) m = fmaxf(m, ml[s].x);
-    const float m_use = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    bool absent = true;
-    for (int s = 0; s < n_splits; s++) {
-        const float w = amx_exp2(ml[s].x - m_use);
-        const float4 o = *reinterpret_cast<const float4 *>(part_o + (qrow * n_splits + s) * HD + i);
-        absent = absent && ml[s].y == 0.f;
-        l += w * ml[s].y;
-        x.x += w * o.x; x.y += w * o.y; x.z += w * o.z; x.w += w * o.w;
+// Many queries a K/V head (a tree under grouped heads): a workgroup's waves own 32 queries each and share the keys, in tiles of 64 that they decode
+// together into LDS, each wave 16 rows, a tile ahead of the products (attention_core.h).  Scores run a tile ahead of the values too, so
+// K is decoded two tiles ahead and V one, from codes that were asked for a tile earlier.  A wave finishes its own queries.
+#define AMW_ROWS (32 * AMX_WAVES)
+
+template <int HD, int BITS>
+__global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs a) {
+    using Core = AttnCore<HD>;
+    using Keys = MxKeys<HD, BITS>;
+    constexpr int TILE = Core::TILE, VPL = HD / 4, PARTS = Keys::PARTS;         // values a lane holds of a row: PARTS columns of 8
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];      // K tiles [2], V tiles [2]
+    const int lane = threadIdx.x & 63, hf = lane >> 5, c = lane & 31, g16 = lane >> 4, c16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int Hkv = a.kv.Hkv;
+    int tile, split, b, h;
+    if (!amx_place(a, tile, split, b, h)) return;
+    const int Lc = __builtin_amdgcn_readfirstlane(min(max(a.ctx_len[b], 0), min(a.ctx_hint, a.kv.smax)));
+    const int nq = a.R * a.qpk, qi = tile * AMW_ROWS + wave * 32 + c, qc = min(qi, nq - 1);
+    const bool idle = tile * AMW_ROWS + wave * 32 >= nq;                        // (it decodes all the same)
+    // (a query's row is worked out again where it is needed: kept through the loop it costs registers that are not there)
+    auto row_of = [&](int q) __attribute__((always_inline)) { asm volatile("" : "+v"(q)); return q / a.qpk; };
+    auto query_of = [&](int q, int row) __attribute__((always_inline)) { return ((int64_t)b * a.R + row) * (a.qpk * Hkv) + h * a.qpk + (q - row * a.qpk); };
+
+    Core core;
+    core.init(lane);
+#pragma unroll
+    for (int s = 0; s < Core::KS; s++)
+        core.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(a.q + query_of(qc, row_of(qc)) * HD + 16 * s + 8 * hf));
+
+    const int last_row = min((tile + 1) * AMW_ROWS - 1, nq - 1) / a.qpk;        // of the workgroup: pass rows behind it are nobody's ancestors
+    const int n_c = (Lc + CORE_KEYS - 1) / CORE_KEYS, n_p = (a.P + CORE_KEYS - 1) / CORE_KEYS, n_all = n_c + n_p + last_row / CORE_KEYS + 1;
+    const int begin = split * a.per_split, end = min(n_all, begin + a.per_split), c_end = min(end, n_c);
+
+    const uint32_t lds = (uint32_t)(size_t)((__attribute__((address_space(3))) unsigned char *)smem);
+    auto k_tile = [&](int t) __attribute__((always_inline)) { return lds + (t & 1) * TILE; };
+    auto v_tile = [&](int t) __attribute__((always_inline)) { return lds + 2 * TILE + (t & 1) * TILE; };
+    auto meet = [&]() __attribute__((always_inline)) {                          // what was written to LDS can be read, what was read can be written over
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // This lane decodes row 16 wave + c16 of a tile, values VPL g16 ..: where they go
+    const int my = 16 * wave + c16;
+    uint32_t k_put = my * Core::ROW + (((PARTS * g16) ^ Core::k_swizzle(my)) * 16), v_put = my * Core::ROW + (((PARTS * g16) ^ Core::v_swizzle(my)) * 16);
+    auto put = [&](uint32_t tile, bool is_v, const bf16x8 (&x)[PARTS]) __attribute__((always_inline)) {
+        uint32_t at = tile + (is_v ? v_put : k_put);                            // (a lane's columns sit in address bits that the swizzle shares by exclusive or)
+        asm volatile("" : "+v"(at));
+#pragma unroll
+        for (int s = 0; s < PARTS; s++) *(__attribute__((address_space(3))) u32x4_t *)(uintptr_t)(at ^ (16 * s)) = __builtin_bit_cast(u32x4_t, x[s]);
+    };
+    // (the lane's offsets are worked out where they are used: kept through the loop, 8 bits of 128 spilled)
+    auto lane_now = [&]() __attribute__((always_inline)) {
+        int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    auto first_key = [&](int t) __attribute__((always_inline)) { return t * CORE_KEYS + 16 * wave; };
+    auto load_k = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.k, a.kv.k_scale, h, first_key(t), Lc, page, Keys::code_offset(lane_now()), Keys::scale_offset(lane_now())); };
+    auto load_v = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.v, a.kv.v_scale, h, first_key(t), Lc, page, Keys::code_offset(lane_now()), Keys::scale_offset(lane_now())); };
+    auto page_of = [&](int t) __attribute__((always_inline)) { return Keys::page_of(a.kv, b, first_key(t), Lc); };
+    auto decode = [&](const Keys &x, uint32_t tile, bool is_v) __attribute__((always_inline)) {
+        bf16x8 v[PARTS];
+        x.decode(v);
+        put(tile, is_v, v);
+    };
+    auto decode_k = [&](const Keys &x, int t) __attribute__((always_inline)) { decode(x, k_tile(t), false); };
+    auto decode_v = [&](const Keys &x, int t) __attribute__((always_inline)) { decode(x, v_tile(t), true); };
+    // scores of keys that `sees` has no bit for: none
+    auto mask = [&](f32x16 (&s)[2], uint64_t sees) __attribute__((always_inline)) {
+        sees >>= 4 * hf;
+#pragma unroll
+        for (int e = 0; e < 32; e++) {
+            const uint32_t w = (uint32_t)(sees >> (e & 16 ? 32 : 0));
+            s[e >> 4][e & 15] = w >> (8 * ((e & 15) >> 2) + (e & 3)) & 1 ? s[e >> 4][e & 15] : -INFINITY;
+        }
+    };
+    auto up_to = [](int n) __attribute__((always_inline)) { return n >= 64 ? ~0ull : (1ull << n) - 1; };
+
+    f32x16 s[2];
+    uint32_t p[16], odd = 0;
+    int t = begin;
+    if (t < c_end) {
+        Keys kc, vc;
+        int page = page_of(t), page_next = page_of(t + 1);                      // of the tile whose V, and K, is loaded next
+        load_k(t, page, kc);
+        load_v(t, page, vc);
+        decode_k(kc, t);
+        load_k(t + 1, page_next, kc);                                           // (from here on possibly behind the share's end: never used there)
+        meet();
+        if (!idle) {
+            core.scores(k_tile(t), s);
+            if (t + 1 == n_c) mask(s, up_to(Lc - t * CORE_KEYS));
+            core.take_maximum(core.largest(s), a.scale_log2);                   // (what every query's reference starts with)
+        }
+        page = page_next;
+        page_next = page_of(t + 2);
+        decode_v(vc, t);
+        decode_k(kc, t + 1);
+        load_v(t + 1, page, vc);
+        load_k(t + 2, page_next, kc);
+        for (; t + 1 < c_end; t++) {
+            meet();                                                             // V of tile t and K of t + 1 are there
+            page = page_next;
+            page_next = page_of(t + 3);
+            decode_v(vc, t + 1);
+            decode_k(kc, t + 2);
+            load_v(t + 2, page, vc);
+            load_k(t + 3, page_next, kc);
+            if (idle) continue;
+            f32x16 next[2];
+            core.scores_and_probabilities(k_tile(t + 1), next, s, a.scale_log2, p);
+            core.template add_values<false>(v_tile(t), p, odd);
+            s[0] = next[0];
+            s[1] = next[1];
+            if (t + 2 == n_c) mask(s, up_to(Lc - (t + 1) * CORE_KEYS));
+        }
+        meet();
+        if (!idle) {
+            core.probabilities(s, a.scale_log2, p, false);
+            core.template add_values<false>(v_tile(t), p, odd);
+        }
+        t++;
+    }
+    // ---- the prefix and the pass' rows: bf16, not seen by every query
+    const int t_odd = t, row = row_of(qc);
+    auto rows_of = [&](int t, const uint16_t *&k, const uint16_t *&v, int64_t &ldk, int64_t &ldv, int &n, uint64_t &sees) __attribute__((always_inline)) {
+        const bool in_prefix = t < n_c + n_p;
+        const int key0 = CORE_KEYS * (in_prefix ? t - n_c : t - n_c - n_p);
+        ldk = in_prefix ? HD : a.k_at.row;
+        ldv = in_prefix ? HD : a.v_at.row;
+        k = in_prefix ? a.prompt_k + (int64_t)h * a.P * HD : a.k_rows + a.k_at.at(b, h, 0);
+        v = in_prefix ? a.prompt_v + (int64_t)h * a.P * HD : a.v_rows + a.v_at.at(b, h, 0);
+        k += key0 * ldk;
+        v += key0 * ldv;
+        n = (in_prefix ? a.P : a.R) - key0;
+        sees = (in_prefix ? (a.t.is_mask[row] ? ~0ull : 0) : a.t.anc[(int64_t)row * a.t.words + (key0 >> 6)]) & up_to(n);
+    };
+    for (; t < end; t++) {
+        const uint16_t *k, *v;
+        int64_t ldk, ldv;
+        int n;
+        uint64_t sees;
+        rows_of(t, k, v, ldk, ldv, n, sees);
+        const int r = min(my, n - 1);
+        bf16x8 x[PARTS], y[PARTS];
+#pragma unroll
+        for (int i = 0; i < PARTS; i++) {
+            x[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(k + r * ldk + VPL * g16 + 8 * i));
+            y[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(v + r * ldv + VPL * g16 + 8 * i));
+        }
+        meet();
+        put(k_tile(t), false, x);
+        put(v_tile(t), true, y);
+        meet();
+        if (idle) continue;
+        core.scores(k_tile(t), s);
+        mask(s, sees);
+        core.probabilities(s, a.scale_log2, p, true);
+        core.template add_values<true>(v_tile(t), p, odd);
+    }
+    if (__builtin_amdgcn_ballot_w64(odd != 0) != 0)
+        for (t = t_odd; t < end; t++) {
+            const uint16_t *k, *v;
+            int64_t ldk, ldv;
+            int n;
+            uint64_t sees;
+            rows_of(t, k, v, ldk, ldv, n, sees);
+            core.add_nonfinite(v, ldv, n - 1, sees);
+        }
+
+    if (qi >= nq) return;
+    const int64_t qrow = query_of(qi, row);
+    const float l = core_sum_halves(core.l_run);
+    const bool absent = a.token && !a.t.is_mask[row] && a.token[(int64_t)b * a.R + row] < 0;
+    if (a.n_splits > 1) {                                                       // unnormalised: for attn_mx_merge_kernel
+        // The sum's own power of two goes to the exponent: shares are weighed by what they hold, whatever reference they used (0 for what is no number).
+        const int e = __builtin_amdgcn_frexp_expf(l);
+        float *dst = a.part_o + (qrow * a.n_splits + split) * HD + 4 * hf;
+#pragma unroll
+        for (int n = 0; n < Core::NT; n++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                *reinterpret_cast<float4 *>(dst + 32 * n + 8 * i) =
+                    make_float4(ldexpf(core.o[n][4 * i], -e), ldexpf(core.o[n][4 * i + 1], -e), ldexpf(core.o[n][4 * i + 2], -e), ldexpf(core.o[n][4 * i + 3], -e));
+        if (hf == 0) *reinterpret_cast<float2 *>(a.part_ml + (qrow * a.n_splits + split) * 2) = absent || l == 0.f ? make_float2(-INFINITY, 0.f) : make_float2(core.base + e, ldexpf(l, -e));
+        return;
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    *reinterpret_cast<uint2 *>(out + qrow * HD + i) = absent ? make_uint2(0, 0) : make_uint2(amx_pk_bf16(x.x * inv, x.y * inv), amx_pk_bf16(x.z * inv, x.w * inv));
+    uint16_t *dst = a.out + qrow * HD + 4 * hf;
+#pragma unroll
+    for (int n = 0; n < Core::NT; n++)
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) =
+                absent || l == 0.f ? make_uint2(0, 0) : make_uint2(core_pk_bf16(core.o[n][4 * i] * inv, core.o[n][4 * i + 1] * inv),
+                                                                  core_pk_bf16(core.o[n][4 * i + 2] * inv, core.o[n][4 * i + 3] * inv));
 }
 
-struct AmxPlan { int tiles_u, n_tiles, splits; int64_t workgroups; size_t part_o, part_ml; };
+// o = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max m): HD / 4 threads a query's columns, SIDE such rows of threads side by side its shares (and
+// in a workgroup of 256 or more threads as many queries as there is room for).  A share without keys for the query has m = -inf and is left out
+// (nothing of it need have been written).  Bound by what the shares left in memory.
+template <int HD, int SIDE, int THREADS>
+__global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, int64_t n_queries, int n_splits,
+                                                                uint16_t *__restrict__ out) {
+    constexpr int LANES = HD / 4, QUERIES = THREADS / (LANES * SIDE);
+    const int i = threadIdx.x % LANES, side = threadIdx.x / LANES % SIDE, mine = threadIdx.x / (LANES * SIDE);
+    const int64_t qrow = (int64_t)blockIdx.x * QUERIES + mine;
+    const bool ok = qrow < n_queries;
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (ok ? qrow : 0) * n_splits;
+    const float4 *po = reinterpret_cast<const float4 *>(part_o + (ok ? qrow : 0) * n_splits * HD) + i;
+    float m = -INFINITY, l = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = side; s0 < n_splits; s0 += 4 * SIDE) {                        // four shares of a thread at a time, against their own maximum
+        float2 e[4];
+        float4 o[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int s = min(s0 + k * SIDE, n_splits - 1);
+            e[k] = ml[s];
+            o[k] = po[(int64_t)s * LANES];
+            if (s0 + k * SIDE >= n_splits) e[k].x = -INFINITY;
+        }
+        const float m_new = fmaxf(fmaxf(fmaxf(e[0].x, e[1].x), fmaxf(e[2].x, e[3].x)), m);
+        if (m_new == -INFINITY) continue;
+        const float f = amx_exp2(m - m_new);
+        l *= f;
+        x.x *= f; x.y *= f; x.z *= f; x.w *= f;
+        m = m_new;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if (e[k].x == -INFINITY) continue;
+            const float w = amx_exp2(e[k].x - m);
+            l += w * e[k].y;
+            x.x += w * o[k].x; x.y += w * o[k].y; x.z += w * o[k].z; x.w += w * o[k].w;
+        }
+    }
+    if constexpr (SIDE > 1) {
+        __shared__ float4 s_o[QUERIES][SIDE][LANES];
+        __shared__ float2 s_ml[QUERIES][SIDE];
+        s_o[mine][side][i] = x;
+        if (i == 0) s_ml[mine][side] = make_float2(m, l);
+        __syncthreads();
+        if (side) return;
+        float top = m;
+        for (int k = 1; k < SIDE; k++) top = fmaxf(top, s_ml[mine][k].x);
+        l = 0.f;
+        x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int k = 0; k < SIDE; k++) {
+            const float2 e = s_ml[mine][k];
+            if (e.x == -INFINITY) continue;
+            const float w = amx_exp2(e.x - top);
+            const float4 y = s_o[mine][k][i];
+            l += w * e.y;
+            x.x += w * y.x; x.y += w * y.y; x.z += w * y.z; x.w += w * y.w;
+        }
+        m = top;
+    }
+    if (!ok) return;
+    const float inv = 1.0f / l;
+    *reinterpret_cast<uint2 *>(out + qrow * HD + 4 * i) =
+        m == -INFINITY ? make_uint2(0, 0) : make_uint2(amx_pk_bf16(x.x * inv, x.y * inv), amx_pk_bf16(x.z * inv, x.w * inv));
+}
+template <int HD>
+static void launch_merge(const AmxArgs &a, int64_t queries, int n_splits, hipStream_t s) {
+    // few shares: a thread takes them all; many: 8 or 32 rows of threads share them
+    if (n_splits <= 8) hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 1, 256>), dim3((unsigned)((queries * HD / 4 + 255) / 256)), dim3(256), 0, s, a.part_o, a.part_ml, queries, n_splits, a.out);
+    else if (n_splits <= 32) hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 8, 256>), dim3((unsigned)((queries * HD / 4 * 8 + 255) / 256)), dim3(256), 0, s, a.part_o, a.part_ml, queries, n_splits, a.out);
+    else hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 32, HD * 8>), dim3((unsigned)queries), dim3(HD * 8), 0, s, a.part_o, a.part_ml, queries, n_splits, a.out);
+}
 
-// Queries in tiles of 16, two of them a workgroup where there are two; the keys split until the chip is full or a wave has a chunk or two.
+struct AmxPlan { bool wide; int tiles_u, n_tiles, splits, per_split; int64_t workgroups; size_t part_o, part_ml; };
+
+// How a launch is cut, from nothing but its sizes: one tile of 16 queries a workgroup, two, or 128 queries that share decoded keys (wide); and the keys into
+// shares, which go by the hint, so that shorter sequences of a batch have fewer of them.  The estimate behind the choice, in us at head_dim 128:
+//   a workgroup's start and end, its turns (128 keys, wide 64) at the pace of one workgroup a CU or of as many as a CU holds, and,
+//   where the keys are split, a second kernel and what the shares write and read, at 4.5 TB/s.
+// Measured (one / two tiles / wide): a turn with one workgroup a CU 0.9 / 1.25 / 1.56, with two 1.44 / 2.1 / 2.43; the start and end 5.6 / 5.6 / 7.  The batch's
+// lengths are taken to be three quarters of the hint on average.  32 sequences of up to 8192 keys, 64/8 heads, shares of 4096, 2048, 1365, 1024 keys
+// 45.1, 35.0, 39.1, 38.8 us; 4 sequences of 1024 to 4096, 68 rows (wide) in 2, 3, 4, 5 shares 69.4, 64.7, 58.5, 66.8, in tiles of 32 queries 76;
+// one of 131072 in 47, 61, 79, 94 shares 39.1, 33.5, 36.1, 35.0; one of 1000, 32 heads, in 1, 2, 3, 5, 9 shares 13.6, 11.5, 10.1, 8.8, 8.7.
 static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int ctx_hint, int n_prompt) {
-    AmxPlan p;
-    const int64_t nq = (int64_t)rows * (Hq / Hkv);
-    p.tiles_u = nq > 16 ? 2 : 1;
-    p.n_tiles = (int)((nq + 16 * p.tiles_u - 1) / (16 * p.tiles_u));
-    const int64_t chunks = ((int64_t)n_prompt + AMX_CHUNK - 1) / AMX_CHUNK + ((int64_t)ctx_hint + AMX_CHUNK - 1) / AMX_CHUNK + (rows + AMX_CHUNK - 1) / AMX_CHUNK;
-    const int64_t wgs = (int64_t)batch * Hkv * p.n_tiles;
-    int64_t splits = (512 + wgs - 1) / wgs, most = (chunks + 2 * AMX_WAVES - 1) / (2 * AMX_WAVES);
-    if (splits > most) splits = most;
-    if (splits > 256) splits = 256;
-    if (splits < 1) splits = 1;
-    p.splits = (int)splits;
-    p.workgroups = wgs * splits;
-    const size_t queries = (size_t)batch * rows * Hq;
-    p.part_o = splits > 1 ? (queries * splits * hd * 4 + 255) / 256 * 256 : 0;
-    p.part_ml = splits > 1 ? (queries * splits * 8 + 255) / 256 * 256 : 0;
+    static const struct { int queries, unit, unroll, slots; double start, one, many; } kinds[3] = {
+        {16, AMX_CHUNK, AMX_WAVES, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, AMX_WAVES, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 1, 512, 7.0, 1.56, 2.43}};
+    static const int shares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128, 192, 256};
+    const int64_t nq = (int64_t)rows * (Hq / Hkv), queries = (int64_t)batch * rows * Hq;
+    const double fill = batch > 1 ? 0.75 : 1.0, size = hd / 128.0;
+    AmxPlan p = {};
+    double best = 1e300;
+    for (int k = nq <= 16 ? 0 : 1; k < (nq <= 32 ? (nq <= 16 ? 1 : 2) : 3); k++) {
+        const auto &kind = kinds[k];
+        const int n_tiles = (int)((nq + kind.queries - 1) / kind.queries);
+        auto units = [&](int64_t n) { return (n + kind.unit - 1) / kind.unit; };
+        const int64_t chunks = units(n_prompt) + units(ctx_hint) + units(rows), wgs = (int64_t)batch * Hkv * n_tiles;
+        for (int want : shares) {
+            if (want > 1 && want * kind.unroll > chunks) break;
+            const int64_t turns = (chunks + (int64_t)want * kind.unroll - 1) / ((int64_t)want * kind.unroll), per = turns * kind.unroll, splits = (chunks + per - 1) / per;
+            const double busy = (double)(wgs * splits) * fill;
+            const double rounds = busy <= kind.slots ? 1.0 : batch > 1 ? busy / kind.slots : (double)((int64_t)(busy + kind.slots - 1) / kind.slots);
+            double us = kind.start + rounds * (double)turns * size * (busy <= 256 ? kind.one : kind.many);
+            if (splits > 1) us += 1.5 + 0.03 * (double)splits + (double)(queries * splits) * fill * hd * 8 / 4.5e6;
+            if (us < best) {
+                best = us;
+                p.wide = k == 2;
+                p.tiles_u = k == 0 ? 1 : 2;
+                p.n_tiles = n_tiles;
+                p.splits = (int)splits;
+                p.per_split = (int)per;
+                p.workgroups = wgs * splits;
+            }
+        }
+    }
+    p.part_o = p.splits > 1 ? ((size_t)queries * p.splits * hd * 4 + 255) / 256 * 256 : 0;
+    p.part_ml = p.splits > 1 ? ((size_t)queries * p.splits * 8 + 255) / 256 * 256 : 0;
     return p;
 }
 
@@ -429,11 +749,16 @@ extern "C" int bita_tree_attention_mx_plan_info(int32_t batch, int32_t rows, int
     if (!out4) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_tree_attention_mx_plan_info: null argument");
     if (int rc = amx_sizes("bita_tree_attention_mx_plan_info", batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt)) return rc;
     const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, ctx_hint, n_prompt);
-    out4[0] = p.splits; out4[1] = 16 * p.tiles_u; out4[2] = AMX_WAVES;
+    out4[0] = p.splits; out4[1] = p.wide ? AMW_ROWS : 16 * p.tiles_u; out4[2] = AMX_WAVES;
     out4[3] = p.workgroups < INT32_MAX ? (int32_t)p.workgroups : INT32_MAX;
     return BITA_OK;
 }
 
+template <int HD, int BITS>
+static void launch_amw(const AmxArgs &a, int64_t n_groups, hipStream_t s) {
+    const dim3 grid((unsigned)((n_groups * a.n_splits + 7) / 8 * 8 * a.n_tiles));
+    hipLaunchKernelGGL((attn_mx_wide_kernel<HD, BITS>), grid, dim3(AMX_WAVES * 64), (4 * AttnCore<HD>::TILE), s, a);
+}
 template <int HD, int BITS, int U>
 static void launch_amx(const AmxArgs &a, int64_t n_groups, hipStream_t s) {
     static_assert(AmxCfg<HD, U>::SMEM <= 80 * 1024, "two workgroups a CU");
@@ -465,22 +790,20 @@ extern "C" int bita_tree_attention_mx(const bita_tree_template *t, const void *d
     a.prompt_k = (const uint16_t *)d_prompt_k; a.prompt_v = (const uint16_t *)d_prompt_v;
     a.ctx_len = d_ctx_len; a.token = d_token;
     a.P = n_prompt; a.R = t->dev.rows; a.qpk = n_heads / kv->n_kv_heads; a.ctx_hint = ctx_hint;
-    a.n_tiles = p.n_tiles; a.n_splits = p.splits;
+    a.n_tiles = p.n_tiles; a.n_splits = p.splits; a.per_split = p.per_split;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)kv->head_dim);
     a.part_o = (float *)d_ws; a.part_ml = (float *)((unsigned char *)d_ws + p.part_o);
     a.out = (uint16_t *)d_out;
     hipStream_t s = (hipStream_t)stream;
     const int64_t groups = (int64_t)kv->batch * kv->n_kv_heads;
-#define AMX_LAUNCH(HD_, BITS_) do { if (p.tiles_u == 2) launch_amx<HD_, BITS_, 2>(a, groups, s); else launch_amx<HD_, BITS_, 1>(a, groups, s); } while (0)
+#define AMX_LAUNCH(HD_, BITS_) do { if (p.wide) launch_amw<HD_, BITS_>(a, groups, s); else if (p.tiles_u == 2) launch_amx<HD_, BITS_, 2>(a, groups, s); else launch_amx<HD_, BITS_, 1>(a, groups, s); } while (0)
     if (kv->head_dim == 128) { if (kv->bits == 4) AMX_LAUNCH(128, 4); else AMX_LAUNCH(128, 8); }
     else { if (kv->bits == 4) AMX_LAUNCH(64, 4); else AMX_LAUNCH(64, 8); }
 #undef AMX_LAUNCH
     if (p.splits > 1) {
         const int64_t queries = (int64_t)kv->batch * t->dev.rows * n_heads;
-        const int per_wg = 1024 / kv->head_dim;
-        const dim3 grid((unsigned)((queries + per_wg - 1) / per_wg));
-        if (kv->head_dim == 128) hipLaunchKernelGGL((attn_mx_merge_kernel<128>), grid, dim3(256), 0, s, a.part_o, a.part_ml, queries, p.splits, a.out);
-        else hipLaunchKernelGGL((attn_mx_merge_kernel<64>), grid, dim3(256), 0, s, a.part_o, a.part_ml, queries, p.splits, a.out);
+        if (kv->head_dim == 128) launch_merge<128>(a, queries, p.splits, s);
+        else launch_merge<64>(a, queries, p.splits, s);
     }
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;

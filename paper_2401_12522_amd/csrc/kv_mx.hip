@@ -134,7 +134,7 @@ int kv_mx_of(const bita_kv_mx *kv, KvMx *out, const char *who) {
         return bita_set_error(BITA_ERR_INVALID_ARG, "%s: cache pointers must be multiples of 16 bytes", who);
     if ((kv->bits != 4 && kv->bits != 8) || (kv->head_dim != 64 && kv->head_dim != 128) || kv->n_kv_heads > 65535 || kv->batch > 65535)
         return bita_set_error(BITA_ERR_UNSUPPORTED, "%s: bits 4 or 8, head_dim 64 or 128, at most 65535 heads and sequences", who);
-    *out = KvMx{(unsigned char *)kv->k, (unsigned char *)kv->v, kv->k_scale, kv->v_scale, nullptr, kv->batch, kv->n_kv_heads, kv->smax, 0, 0, 0};
+    *out = KvMx{(unsigned char *)kv->k, (unsigned char *)kv->v, kv->k_scale, kv->v_scale, nullptr, kv->batch, kv->n_kv_heads, kv->smax, 0, kv->smax, -1, kv->batch, 0};
     if (!kv->block_table) return BITA_OK;
     const int ps = kv->page_size;
     if (ps < 16 || (ps & (ps - 1)) || kv->n_pages <= 0 || kv->max_pages <= 0)
@@ -143,6 +143,8 @@ int kv_mx_of(const bita_kv_mx *kv, KvMx *out, const char *who) {
         return bita_set_error(BITA_ERR_CAPACITY, "%s: smax %d exceeds the block table (%d pages of %d)", who, kv->smax, kv->max_pages, ps);
     out->table = kv->block_table;
     out->page_lg = __builtin_ctz((unsigned)ps);
+    out->page_rows = ps;
+    out->slot_mask = ps - 1;
     out->n_pages = kv->n_pages;
     out->max_pages = kv->max_pages;
     return BITA_OK;

@@ -5,15 +5,14 @@
 struct KvMx {
     unsigned char *k, *v;
     uint8_t *k_scale, *v_scale;
-    const int32_t *table;               // nullptr: contiguous
-    int batch, Hkv, smax, page_lg, n_pages, max_pages;
+    const int32_t *table;               // nullptr: contiguous, a sequence a page
+    int batch, Hkv, smax, page_lg, page_rows, slot_mask, n_pages, max_pages;
 };
 
 // Row of slot j of (sequence, head): codes at row * HD * BITS / 8, scales at row * HD / 32.
 __device__ __forceinline__ int64_t mx_row(const KvMx &kv, int b, int h, int j) {
-    if (!kv.table) return ((int64_t)b * kv.Hkv + h) * kv.smax + j;
-    const int page = min(max(kv.table[(int64_t)b * kv.max_pages + (j >> kv.page_lg)], 0), kv.n_pages - 1);
-    return (((int64_t)page * kv.Hkv + h) << kv.page_lg) + (j & ((1 << kv.page_lg) - 1));
+    const int page = kv.table ? min(max(kv.table[(int64_t)b * kv.max_pages + (j >> kv.page_lg)], 0), kv.n_pages - 1) : b;
+    return ((int64_t)page * kv.Hkv + h) * kv.page_rows + (j & kv.slot_mask);
 }
 
 // The scale byte of a block whose largest magnitude has these fp32 bits (NaN and infinity: 255, as integers they are above the rest).

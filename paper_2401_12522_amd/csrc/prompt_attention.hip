@@ -73,7 +73,7 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void prompt_attn_kernel(PromptArg
     using Core = AttnCore<HD>;
     constexpr int KS = Core::KS, NT = Core::NT, TILE = Core::TILE, GPR = HD / 8, RPI = 64 / GPR;    // granules a row, rows a load instruction
     constexpr int LOADS = CORE_KEYS / RPI / PA_WAVES;                                   // load instructions of a wave, K or V tile
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];                // K tiles [2], V tiles [2]
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];              // K tiles [2], V tiles [2]
     const int lane = threadIdx.x & 63, hf = lane >> 5, c = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j = blockIdx.x % a.Hq;
