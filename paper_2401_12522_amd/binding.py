@@ -723,30 +723,37 @@ def gemm_q8(a, a_scale, w_packed, w_scale, n_rows, out=None, out_dtype=torch.flo
 
 
 # ---- a K/V cache in 4 or 8 bits, and the attention block around it ------------------------------------------------------------
-_BF16 = {torch.bfloat16: 1}
+# (Called for every layer of a pass: a tensor is asked for each thing once, messages are made up only for what is refused.)
+_BF16, _I32, _U8, _F32 = {torch.bfloat16: 1}, {torch.int32: 0}, {torch.uint8: 0}, {torch.float32: 0}
 
 
-def _tensor(name, t, types, dev, shape):
-    """Strides of t, a tensor of one of these types and this shape (None: any extent) on the current device, neighbouring elements last."""
-    if t.dtype in types and t.get_device() == dev and t.dim() == len(shape):
-        for have, want in zip(t.shape, shape):
-            if want is not None and have != want:
-                break
-        else:
-            s = t.stride()
-            if s[-1] == 1:
-                return s if 1 not in t.shape else tuple(0 if n == 1 else st for n, st in zip(t.shape, s))
-    raise ValueError(f"{name}: wanted {' x '.join('any' if n is None else str(n) for n in shape)} of {' or '.join(str(x) for x in types)} on cuda:{dev}, "
-                     f"last dimension contiguous; got {tuple(t.shape)} of {t.dtype} on {t.device}, strides {tuple(t.stride())}")
+def _refuse(name, t, types, dev, shape, what="last dimension contiguous"):
+    raise ValueError(f"{name}: wanted {' x '.join('any' if n is None else str(n) for n in shape)} of {' or '.join(str(x) for x in types)} on cuda:{dev}, {what}; "
+                     f"got {tuple(t.shape)} of {t.dtype} on {t.device}, strides {tuple(t.stride())}")
+
+
+def _strides(name, t, types, dev, shape):
+    """Strides of t, a tensor of one of these types and of this shape on the current device, neighbouring elements last."""
+    if t.dtype in types and t.shape == shape and t.get_device() == dev:
+        s = t.stride()
+        if s[-1] == 1:
+            return s
+    _refuse(name, t, types, dev, shape)
 
 
 def _dense(name, t, types, dev, shape):
-    _tensor(name, t, types, dev, shape)
-    if not t.is_contiguous():
-        raise ValueError(f"{name}: wanted a contiguous tensor; got strides {tuple(t.stride())}")
+    """The same of a contiguous tensor; its address."""
+    if t.dtype in types and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(name, t, types, dev, shape, "contiguous")
 
 
-_I32, _U8, _F32 = {torch.int32: 0}, {torch.uint8: 0}, {torch.float32: 0}
+def _shape(name, t, n):
+    """Extents of a tensor of n dimensions."""
+    shape = t.shape
+    if len(shape) != n:
+        raise ValueError(f"{name}: wanted {n} dimensions; got {tuple(shape)}")
+    return shape
 
 
 class KVCacheMX:
@@ -762,8 +769,8 @@ class KVCacheMX:
             raise ValueError(f"KVCacheMX: bits 4 or 8, head_dim 64 or 128 and positive sizes wanted; got {bits}, {head_dim}, {(n_kv_heads, batch, smax)}")
         self.block_table, self.page_size, self.max_pages, self.n_pages = block_table, 0, 0, 0
         if block_table is not None:
-            _dense("block_table", block_table, _I32, dev, (self.batch, None))
-            self.page_size, self.max_pages = int(page_size), block_table.shape[1]
+            self.page_size, self.max_pages = int(page_size), _shape("block_table", block_table, 2)[1]
+            _dense("block_table", block_table, _I32, dev, (self.batch, self.max_pages))
             if self.page_size < 16 or self.page_size & (self.page_size - 1) or self.smax > self.max_pages * self.page_size:
                 raise ValueError(f"KVCacheMX: page_size a power of two >= 16 and smax <= {self.max_pages} pages of it wanted; got {page_size}, {smax}")
             self.n_pages = int(n_pages) if n_pages is not None else k.shape[0] if k is not None else self.batch * self.max_pages
@@ -792,25 +799,24 @@ def kv_write_mx(cache, k, v, start, count=None, path=None, cu_rows=None):
     (int32 [B+1]) packed [T][Hkv][hd].  start, count: int32 [B]; count None: all rows.  path int32 [B][m]: row i is k[b, :, path[b, i]]
     (accept's path, with count its n_acc).  No length is changed."""
     L, dev = _lib or lib(), torch.cuda.current_device()
-    ref, B, H, D = cache.on(dev), cache.batch, cache.n_kv_heads, cache.head_dim
-    seq = vseq = 0
+    ref, B, H, D, dtype = cache.on(dev), cache.batch, cache.n_kv_heads, cache.head_dim, k.dtype
+    seq = vseq = pcount = ppath = m = pcu = 0
     if cu_rows is not None:
-        n = k.shape[0]
-        row, head, _ = _tensor("k", k, _F32_BF16, dev, (None, H, D))
-        vrow, vhead, _ = _tensor("v", v, {k.dtype: 0}, dev, (n, H, D))
-        _vector("cu_rows", cu_rows, B + 1, torch.int32, dev)
+        n = _shape("k", k, 3)[0]
+        row, head, _ = _strides("k", k, _F32_BF16, dev, (n, H, D))
+        vrow, vhead, _ = _strides("v", v, {dtype}, dev, (n, H, D))
+        pcu = _dense("cu_rows", cu_rows, _I32, dev, (B + 1,))
     else:
-        seq, head, row, _ = _tensor("k", k, _F32_BF16, dev, (B, H, None, D))
-        n = k.shape[2]
-        vseq, vhead, vrow, _ = _tensor("v", v, {k.dtype: 0}, dev, (B, H, n, D))
-    _vector("start", start, B, torch.int32, dev)
+        n = _shape("k", k, 4)[2]
+        seq, head, row, _ = _strides("k", k, _F32_BF16, dev, (B, H, n, D))
+        vseq, vhead, vrow, _ = _strides("v", v, {dtype}, dev, (B, H, n, D))
     if count is not None:
-        _vector("count", count, B, torch.int32, dev)
+        pcount = _dense("count", count, _I32, dev, (B,))
     if path is not None:
-        _dense("path", path, _I32, dev, (B, None))
-    rc = L.bita_kv_write_mx(ref, k.data_ptr(), seq, head, row, v.data_ptr(), vseq, vhead, vrow, _F32_BF16[k.dtype], n, start.data_ptr(), count.data_ptr() if count is not None else None,
-                            path.data_ptr() if path is not None else None, path.shape[1] if path is not None else 0,
-                            cu_rows.data_ptr() if cu_rows is not None else None, _raw_stream(dev))
+        m = _shape("path", path, 2)[1]
+        ppath = _dense("path", path, _I32, dev, (B, m))
+    rc = L.bita_kv_write_mx(ref, k.data_ptr(), seq, head, row, v.data_ptr(), vseq, vhead, vrow, _F32_BF16[dtype], n, _dense("start", start, _I32, dev, (B,)), pcount, ppath, m,
+                            pcu, _raw_stream(dev))
     if rc:
         _check(rc)
 
@@ -820,14 +826,18 @@ def kv_read_mx(cache, k, v, length, start=None):
     exact in either; one of them may be None).  start, length: int32 [B]; start None: 0.  What lies behind a length is left as it is."""
     L, dev = _lib or lib(), torch.cuda.current_device()
     ref, one = cache.on(dev), k if k is not None else v
-    seq, head, row, _ = vseq, vhead, vrow, _ = _tensor("k" if k is not None else "v", one, _F32_BF16, dev, (cache.batch, cache.n_kv_heads, None, cache.head_dim))
-    if v is not None and k is not None:
-        vseq, vhead, vrow, _ = _tensor("v", v, {k.dtype: 0}, dev, k.shape)
-    _vector("length", length, cache.batch, torch.int32, dev)
+    B, dtype, n = cache.batch, one.dtype, _shape("k" if k is not None else "v", one, 4)[2]
+    shape = (B, cache.n_kv_heads, n, cache.head_dim)
+    seq = head = row = vseq = vhead = vrow = pk = pv = pstart = 0
+    if k is not None:
+        seq, head, row, _ = _strides("k", k, _F32_BF16, dev, shape)
+        pk = k.data_ptr()
+    if v is not None:
+        vseq, vhead, vrow, _ = _strides("v", v, {dtype} if k is not None else _F32_BF16, dev, shape)
+        pv = v.data_ptr()
     if start is not None:
-        _vector("start", start, cache.batch, torch.int32, dev)
-    rc = L.bita_kv_read_mx(ref, k.data_ptr() if k is not None else None, seq, head, row, v.data_ptr() if v is not None else None, vseq, vhead, vrow,
-                           _F32_BF16[one.dtype], one.shape[2], start.data_ptr() if start is not None else None, length.data_ptr(), _raw_stream(dev))
+        pstart = _dense("start", start, _I32, dev, (B,))
+    rc = L.bita_kv_read_mx(ref, pk, seq, head, row, pv, vseq, vhead, vrow, _F32_BF16[dtype], n, pstart, _dense("length", length, _I32, dev, (B,)), _raw_stream(dev))
     if rc:
         _check(rc)
 
@@ -838,28 +848,29 @@ def qk_norm_rope(x, pos, cos, sin, n_heads, n_kv_heads, q_gain=None, k_gain=None
     Returns (q [M][n_heads][hd], k [M][n_kv_heads][hd], v) in bfloat16, written into q, k, v where they are given (they may be views of a
     bfloat16 x's own columns).  v: x's rounded to bfloat16; where x is bfloat16 and no v is given, a view of x."""
     L, dev = _lib or lib(), torch.cuda.current_device()
-    max_pos, half = cos.shape
-    hd = 2 * half
+    max_pos, half = table = _shape("cos", cos, 2)
+    hd, bf16 = 2 * half, torch.bfloat16
     m, _, ldx = _matrix("x", x, _F32_BF16, dev, None, (n_heads + 2 * n_kv_heads) * hd)
-    _dense("cos", cos, _F32, dev, (None, None))
-    _dense("sin", sin, _F32, dev, (max_pos, half))
-    _vector("pos", pos, m, torch.int32, dev)
-    for name, t in (("q_gain", q_gain), ("k_gain", k_gain)):
-        if t is not None:
-            _vector(name, t, hd, torch.bfloat16, dev)
-    q = torch.empty((m, n_heads, hd), dtype=torch.bfloat16, device=x.device) if q is None else q
-    k = torch.empty((m, n_kv_heads, hd), dtype=torch.bfloat16, device=x.device) if k is None else k
-    (ldq, hq, _), (ldk, hk, _) = _tensor("q", q, _BF16, dev, (m, n_heads, hd)), _tensor("k", k, _BF16, dev, (m, n_kv_heads, hd))
-    pv = ldv = hv = 0
-    if v is None and x.dtype is torch.bfloat16:
+    dtype, pqg, pkg, pv, ldv, hv = x.dtype, 0, 0, 0, 0, 0
+    if q_gain is not None:
+        pqg = _dense("q_gain", q_gain, _BF16, dev, (hd,))
+    if k_gain is not None:
+        pkg = _dense("k_gain", k_gain, _BF16, dev, (hd,))
+    if q is None:
+        q = x.new_empty((m, n_heads, hd), dtype=bf16)
+    if k is None:
+        k = x.new_empty((m, n_kv_heads, hd), dtype=bf16)
+    (ldq, hq, _), (ldk, hk, _) = _strides("q", q, _BF16, dev, (m, n_heads, hd)), _strides("k", k, _BF16, dev, (m, n_kv_heads, hd))
+    if v is None and dtype is bf16:
         v = x[:, (n_heads + n_kv_heads) * hd:].unflatten(1, (n_kv_heads, hd))
     else:
-        v = torch.empty((m, n_kv_heads, hd), dtype=torch.bfloat16, device=x.device) if v is None else v
-        ldv, hv, _ = _tensor("v", v, _BF16, dev, (m, n_kv_heads, hd))
+        if v is None:
+            v = x.new_empty((m, n_kv_heads, hd), dtype=bf16)
+        ldv, hv, _ = _strides("v", v, _BF16, dev, (m, n_kv_heads, hd))
         pv = v.data_ptr()
-    rc = L.bita_qk_norm_rope(x.data_ptr(), _F32_BF16[x.dtype], m, ldx, n_heads, n_kv_heads, hd, q_gain.data_ptr() if q_gain is not None else None,
-                             k_gain.data_ptr() if k_gain is not None else None, eps, pos.data_ptr(), cos.data_ptr(), sin.data_ptr(), max_pos, q.data_ptr(), ldq, hq,
-                             k.data_ptr(), ldk, hk, pv, ldv, hv, _raw_stream(dev))
+    rc = L.bita_qk_norm_rope(x.data_ptr(), _F32_BF16[dtype], m, ldx, n_heads, n_kv_heads, hd, pqg, pkg, eps, _dense("pos", pos, _I32, dev, (m,)),
+                             _dense("cos", cos, _F32, dev, table), _dense("sin", sin, _F32, dev, table), max_pos, q.data_ptr(), ldq, hq, k.data_ptr(), ldk, hk, pv, ldv, hv,
+                             _raw_stream(dev))
     if rc:
         _check(rc)
     return q, k, v
@@ -884,35 +895,32 @@ def tree_attention_mx(tmpl, q, cache, k_rows, v_rows, ctx_len, ctx_hint, prompt_
     workspace: uint8 cuda of bita_tree_attention_mx_workspace_bytes (allocated here when it is None and one is needed)."""
     L, dev = _lib or lib(), torch.cuda.current_device()
     ref, B, H, D, R = cache.on(dev), cache.batch, cache.n_kv_heads, cache.head_dim, tmpl.rows
-    _dense("q", q, _BF16, dev, (B, R, None, D))
-    Hq, ctx_hint = q.shape[2], int(ctx_hint)
-    seq, head, row, _ = _tensor("k_rows", k_rows, _BF16, dev, (B, H, R, D))
-    vseq, vhead, vrow, _ = _tensor("v_rows", v_rows, _BF16, dev, (B, H, R, D))
-    P = pk = pv = 0
+    Hq, ctx_hint = _shape("q", q, 4)[2], int(ctx_hint)
+    seq, head, row, _ = _strides("k_rows", k_rows, _BF16, dev, (B, H, R, D))
+    vseq, vhead, vrow, _ = _strides("v_rows", v_rows, _BF16, dev, (B, H, R, D))
+    P = pk = pv = pt = pw = nw = 0
     if prompt_k is not None:
-        P = prompt_k.shape[1]
-        _dense("prompt_k", prompt_k, _BF16, dev, (H, None, D))
-        _dense("prompt_v", prompt_v, _BF16, dev, (H, P, D))
-        pk, pv = prompt_k.data_ptr(), prompt_v.data_ptr()
-    _vector("ctx_len", ctx_len, B, torch.int32, dev)
+        P = _shape("prompt_k", prompt_k, 3)[1]
+        pk, pv = _dense("prompt_k", prompt_k, _BF16, dev, (H, P, D)), _dense("prompt_v", prompt_v, _BF16, dev, (H, P, D))
     if token is not None:
-        _dense("token", token, _I32, dev, (B, R))
+        pt = _dense("token", token, _I32, dev, (B, R))
+    pq = _dense("q", q, _BF16, dev, (B, R, Hq, D))
     if out is None:
-        out = torch.empty((B, R, Hq * D), dtype=torch.bfloat16, device=q.device)
+        out = q.new_empty((B, R, Hq * D))
+        po = out.data_ptr()
     else:
-        _dense("out", out, _BF16, dev, (B, R, Hq * D))
-    pw = nw = 0
+        po = _dense("out", out, _BF16, dev, (B, R, Hq * D))
     if workspace is None:
         nw = _attention_mx_scratch(B, R, Hq, H, D, cache.bits, ctx_hint, P)
         if nw:
-            workspace = torch.empty(nw, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(nw, dtype=torch.uint8)
     else:
         _bytes("workspace", workspace, 0, dev)
         nw = workspace.numel()
     if nw:
         pw = workspace.data_ptr()
-    rc = L.bita_tree_attention_mx(tmpl.handle, q.data_ptr(), ref, k_rows.data_ptr(), seq, head, row, v_rows.data_ptr(), vseq, vhead, vrow, pk, pv, P, ctx_len.data_ptr(),
-                                  token.data_ptr() if token is not None else None, Hq, ctx_hint, pw, nw, out.data_ptr(), _raw_stream(dev))
+    rc = L.bita_tree_attention_mx(tmpl.handle, pq, ref, k_rows.data_ptr(), seq, head, row, v_rows.data_ptr(), vseq, vhead, vrow, pk, pv, P,
+                                  _dense("ctx_len", ctx_len, _I32, dev, (B,)), pt, Hq, ctx_hint, pw, nw, po, _raw_stream(dev))
     if rc:
         _check(rc)
     return out
@@ -923,20 +931,18 @@ def prompt_attention(q, k, v, cu_seqlens, out=None):
     own); sequence b is rows cu_seqlens[b] .. cu_seqlens[b+1]-1 (int32 cuda [B+1]).  Returns bfloat16 [T][Hq*hd], written into out where it is
     given; rows outside the sequences are left as they are (undefined where out is allocated here)."""
     L, dev = _lib or lib(), torch.cuda.current_device()
-    ldq, hq, _ = _tensor("q", q, _BF16, dev, (None, None, None))
-    T, Hq, D = q.shape
-    ldk, hk, _ = _tensor("k", k, _BF16, dev, (T, None, D))
-    H = k.shape[1]
-    ldv, hv, _ = _tensor("v", v, _BF16, dev, (T, H, D))
+    T, Hq, D = shape = _shape("q", q, 3)
+    H = _shape("k", k, 3)[1]
+    ldq, hq, _ = _strides("q", q, _BF16, dev, shape)
+    ldk, hk, _ = _strides("k", k, _BF16, dev, (T, H, D))
+    ldv, hv, _ = _strides("v", v, _BF16, dev, (T, H, D))
     n = cu_seqlens.numel()
-    _vector("cu_seqlens", cu_seqlens, n, torch.int32, dev)
     if out is None:
-        out = torch.empty((T, Hq * D), dtype=torch.bfloat16, device=q.device)
-    ldo = _tensor("out", out, _BF16, dev, (T, Hq * D))[0]
-    if T == 1:
-        ldo = Hq * D
-    rc = L.bita_prompt_attention(q.data_ptr(), ldq, hq, k.data_ptr(), ldk, hk, v.data_ptr(), ldv, hv, cu_seqlens.data_ptr(), n - 1, T, Hq, H, D, out.data_ptr(),
-                                 ldo, _raw_stream(dev))
+        out, ldo = q.new_empty((T, Hq * D)), Hq * D
+    else:
+        ldo = _strides("out", out, _BF16, dev, (T, Hq * D))[0]
+    rc = L.bita_prompt_attention(q.data_ptr(), ldq, hq, k.data_ptr(), ldk, hk, v.data_ptr(), ldv, hv, _dense("cu_seqlens", cu_seqlens, _I32, dev, (n,)), n - 1, T, Hq, H, D,
+                                 out.data_ptr(), ldo, _raw_stream(dev))
     if rc:
         _check(rc)
     return out

@@ -106,20 +106,20 @@ struct MxKeys {
     }
 };
 
-template <int HD, int U>
+template <int HD, int U, int W>
 struct AmxCfg {
     static constexpr int KS = HD / 32, NT = HD / 16, VPL = HD / 4;      // k-steps, 16-wide tiles of the head, values a lane holds of a key
     static constexpr int V_BYTES = AMX_CHUNK * HD * 2;                  // a wave's V chunk as bf16
-    static constexpr int MERGE = U * AMX_WAVES * NT * 64 * 16;
-    static constexpr int ML = AMX_WAVES * V_BYTES > MERGE ? AMX_WAVES * V_BYTES : MERGE;
-    static constexpr int SMEM = ML + 2 * U * AMX_WAVES * 16 * 4;
+    static constexpr int MERGE = U * W * NT * 64 * 16;
+    static constexpr int ML = W * V_BYTES > MERGE ? W * V_BYTES : MERGE;
+    static constexpr int SMEM = ML + 2 * U * W * 16 * 4;
 };
 
-template <int HD, int BITS, int U>
-__global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_kernel(AmxArgs a) {
-    using C = AmxCfg<HD, U>;
+template <int HD, int BITS, int U, int W>
+__global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
+    using C = AmxCfg<HD, U, W>;
     using Keys = MxKeys<HD, BITS>;
-    constexpr int KS = C::KS, NT = C::NT, VPL = C::VPL, W = AMX_WAVES;
+    constexpr int KS = C::KS, NT = C::NT, VPL = C::VPL;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -682,7 +682,7 @@ static void launch_merge(const AmxArgs &a, int64_t queries, int n_splits, hipStr
     else hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 32, HD * 8>), dim3((unsigned)queries), dim3(HD * 8), 0, s, a.part_o, a.part_ml, queries, n_splits, a.out);
 }
 
-struct AmxPlan { bool wide; int tiles_u, n_tiles, splits, per_split; int64_t workgroups; size_t part_o, part_ml; };
+struct AmxPlan { bool wide; int tiles_u, waves, n_tiles, splits, per_split; int64_t workgroups; size_t part_o, part_ml; };
 
 // How a launch is cut, from nothing but its sizes: one tile of 16 queries a workgroup, two, or 128 queries that share decoded keys (wide); and the keys into
 // shares, which go by the hint, so that shorter sequences of a batch have fewer of them.  The estimate behind the choice, in us at head_dim 128:
@@ -693,29 +693,31 @@ struct AmxPlan { bool wide; int tiles_u, n_tiles, splits, per_split; int64_t wor
 // 45.1, 35.0, 39.1, 38.8 us; 4 sequences of 1024 to 4096, 68 rows (wide) in 2, 3, 4, 5 shares 69.4, 64.7, 58.5, 66.8, in tiles of 32 queries 76;
 // one of 131072 in 47, 61, 79, 94 shares 39.1, 33.5, 36.1, 35.0; one of 1000, 32 heads, in 1, 2, 3, 5, 9 shares 13.6, 11.5, 10.1, 8.8, 8.7.
 static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int ctx_hint, int n_prompt) {
-    static const struct { int queries, unit, unroll, slots; double start, one, many; } kinds[3] = {
-        {16, AMX_CHUNK, AMX_WAVES, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, AMX_WAVES, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 1, 512, 7.0, 1.56, 2.43}};
+    static const struct { int queries, unit, waves, slots; double start, one, many; } kinds[4] = {
+        {16, AMX_CHUNK, 8, 256, 5.6, 1.0, 1.0}, {16, AMX_CHUNK, 4, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, 4, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 4, 512, 7.0, 1.56, 2.43}};
     static const int shares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128, 192, 256};
     const int64_t nq = (int64_t)rows * (Hq / Hkv), queries = (int64_t)batch * rows * Hq;
     const double fill = batch > 1 ? 0.75 : 1.0, size = hd / 128.0;
     AmxPlan p = {};
     double best = 1e300;
-    for (int k = nq <= 16 ? 0 : 1; k < (nq <= 32 ? (nq <= 16 ? 1 : 2) : 3); k++) {
+    for (int k = nq <= 16 ? 0 : 2; k < (nq <= 16 ? 2 : nq <= 32 ? 3 : 4); k++) {
         const auto &kind = kinds[k];
+        const int unroll = k == 3 ? 1 : kind.waves;                             // chunks of a turn
         const int n_tiles = (int)((nq + kind.queries - 1) / kind.queries);
         auto units = [&](int64_t n) { return (n + kind.unit - 1) / kind.unit; };
         const int64_t chunks = units(n_prompt) + units(ctx_hint) + units(rows), wgs = (int64_t)batch * Hkv * n_tiles;
         for (int want : shares) {
-            if (want > 1 && want * kind.unroll > chunks) break;
-            const int64_t turns = (chunks + (int64_t)want * kind.unroll - 1) / ((int64_t)want * kind.unroll), per = turns * kind.unroll, splits = (chunks + per - 1) / per;
+            if (want > 1 && want * unroll > chunks) break;
+            const int64_t turns = (chunks + (int64_t)want * unroll - 1) / ((int64_t)want * unroll), per = turns * unroll, splits = (chunks + per - 1) / per;
             const double busy = (double)(wgs * splits) * fill;
             const double rounds = busy <= kind.slots ? 1.0 : batch > 1 ? busy / kind.slots : (double)((int64_t)(busy + kind.slots - 1) / kind.slots);
             double us = kind.start + rounds * (double)turns * size * (busy <= 256 ? kind.one : kind.many);
-            if (splits > 1) us += 1.5 + 0.03 * (double)splits + (double)(queries * splits) * fill * hd * 8 / 4.5e6;
+            if (splits > 1) us += 2.5 + 0.03 * (double)splits + (double)(queries * splits) * fill * hd * 8 / 4.5e6;
             if (us < best) {
                 best = us;
-                p.wide = k == 2;
-                p.tiles_u = k == 0 ? 1 : 2;
+                p.wide = k == 3;
+                p.tiles_u = k < 2 ? 1 : 2;
+                p.waves = kind.waves;
                 p.n_tiles = n_tiles;
                 p.splits = (int)splits;
                 p.per_split = (int)per;
@@ -749,7 +751,7 @@ extern "C" int bita_tree_attention_mx_plan_info(int32_t batch, int32_t rows, int
     if (!out4) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_tree_attention_mx_plan_info: null argument");
     if (int rc = amx_sizes("bita_tree_attention_mx_plan_info", batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt)) return rc;
     const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, ctx_hint, n_prompt);
-    out4[0] = p.splits; out4[1] = p.wide ? AMW_ROWS : 16 * p.tiles_u; out4[2] = AMX_WAVES;
+    out4[0] = p.splits; out4[1] = p.wide ? AMW_ROWS : 16 * p.tiles_u; out4[2] = p.waves;
     out4[3] = p.workgroups < INT32_MAX ? (int32_t)p.workgroups : INT32_MAX;
     return BITA_OK;
 }
@@ -759,12 +761,13 @@ static void launch_amw(const AmxArgs &a, int64_t n_groups, hipStream_t s) {
     const dim3 grid((unsigned)((n_groups * a.n_splits + 7) / 8 * 8 * a.n_tiles));
     hipLaunchKernelGGL((attn_mx_wide_kernel<HD, BITS>), grid, dim3(AMX_WAVES * 64), (4 * AttnCore<HD>::TILE), s, a);
 }
-template <int HD, int BITS, int U>
+template <int HD, int BITS, int U, int W>
 static void launch_amx(const AmxArgs &a, int64_t n_groups, hipStream_t s) {
-    static_assert(AmxCfg<HD, U>::SMEM <= 80 * 1024, "two workgroups a CU");
-    (void)hipFuncSetAttribute((const void *)attn_mx_kernel<HD, BITS, U>, hipFuncAttributeMaxDynamicSharedMemorySize, AmxCfg<HD, U>::SMEM);
+    constexpr int SMEM = AmxCfg<HD, U, W>::SMEM;
+    static_assert(W / AMX_WAVES * SMEM <= 160 * 1024 && SMEM <= 80 * 1024, "two workgroups a CU");
+    if (SMEM > 64 * 1024) (void)hipFuncSetAttribute((const void *)attn_mx_kernel<HD, BITS, U, W>, hipFuncAttributeMaxDynamicSharedMemorySize, SMEM);
     const dim3 grid((unsigned)((n_groups * a.n_splits + 7) / 8 * 8 * a.n_tiles));
-    hipLaunchKernelGGL((attn_mx_kernel<HD, BITS, U>), grid, dim3(AMX_WAVES * 64), (AmxCfg<HD, U>::SMEM), s, a);
+    hipLaunchKernelGGL((attn_mx_kernel<HD, BITS, U, W>), grid, dim3(W * 64), SMEM, s, a);
 }
 
 extern "C" int bita_tree_attention_mx(const bita_tree_template *t, const void *d_q, const bita_kv_mx *kv, const void *d_k_rows, int64_t k_seq, int64_t k_head,
@@ -778,8 +781,8 @@ extern "C" int bita_tree_attention_mx(const bita_tree_template *t, const void *d
     if (int rc = kv_mx_of(kv, &a.kv, who)) return rc;
     if (int rc = amx_sizes(who, kv->batch, t->dev.rows, n_heads, kv->n_kv_heads, kv->head_dim, kv->bits, ctx_hint, n_prompt)) return rc;
     if (ctx_hint > kv->smax) return bita_set_error(BITA_ERR_CAPACITY, "%s: ctx_hint %d outside capacity %d", who, ctx_hint, kv->smax);
-    a.k_at = MxRows{k_seq, k_head, k_row};
-    a.v_at = MxRows{v_seq, v_head, v_row};
+    a.k_at = mx_rows(kv->batch, k_seq, kv->n_kv_heads, k_head, t->dev.rows, k_row);
+    a.v_at = mx_rows(kv->batch, v_seq, kv->n_kv_heads, v_head, t->dev.rows, v_row);
     if (int rc = mx_rows_check(who, a.k_at, a.v_at, (uintptr_t)d_q | (uintptr_t)d_k_rows | (uintptr_t)d_v_rows | (uintptr_t)d_prompt_k | (uintptr_t)d_prompt_v |
                                                         (uintptr_t)d_out | (uintptr_t)d_ws)) return rc;
     const AmxPlan p = amx_plan(kv->batch, t->dev.rows, n_heads, kv->n_kv_heads, kv->head_dim, ctx_hint, n_prompt);
@@ -796,7 +799,8 @@ extern "C" int bita_tree_attention_mx(const bita_tree_template *t, const void *d
     a.out = (uint16_t *)d_out;
     hipStream_t s = (hipStream_t)stream;
     const int64_t groups = (int64_t)kv->batch * kv->n_kv_heads;
-#define AMX_LAUNCH(HD_, BITS_) do { if (p.wide) launch_amw<HD_, BITS_>(a, groups, s); else if (p.tiles_u == 2) launch_amx<HD_, BITS_, 2>(a, groups, s); else launch_amx<HD_, BITS_, 1>(a, groups, s); } while (0)
+#define AMX_LAUNCH(HD_, BITS_) do { if (p.wide) launch_amw<HD_, BITS_>(a, groups, s); else if (p.tiles_u == 2) launch_amx<HD_, BITS_, 2, 4>(a, groups, s); \
+    else if (p.waves == 8) launch_amx<HD_, BITS_, 1, 8>(a, groups, s); else launch_amx<HD_, BITS_, 1, 4>(a, groups, s); } while (0)
     if (kv->head_dim == 128) { if (kv->bits == 4) AMX_LAUNCH(128, 4); else AMX_LAUNCH(128, 8); }
     else { if (kv->bits == 4) AMX_LAUNCH(64, 4); else AMX_LAUNCH(64, 8); }
 #undef AMX_LAUNCH

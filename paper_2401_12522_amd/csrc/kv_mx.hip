@@ -178,8 +178,9 @@ extern "C" int bita_kv_write_mx(const bita_kv_mx *kv, const void *d_k, int64_t k
     if (d_path && (d_cu_rows || path_stride <= 0 || path_stride > MX_MAX_ROWS))
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_kv_write_mx: a path has a positive length and goes with rows by sequence");
     KvMx c;
-    const MxRows ks = {k_seq, k_head, k_row}, vs = {v_seq, v_head, v_row};
     if (int rc = kv_mx_of(kv, &c, "bita_kv_write_mx")) return rc;
+    const MxRows ks = mx_rows(d_cu_rows ? 1 : kv->batch, k_seq, kv->n_kv_heads, k_head, n_rows, k_row),
+                 vs = mx_rows(d_cu_rows ? 1 : kv->batch, v_seq, kv->n_kv_heads, v_head, n_rows, v_row);
     if (int rc = check_rows("bita_kv_write_mx", type, n_rows, ks, vs, d_k, d_v)) return rc;
     if (n_rows == 0) return BITA_OK;
     const int per_wg = MX_THREADS * 8 / kv->head_dim;
@@ -195,8 +196,8 @@ extern "C" int bita_kv_read_mx(const bita_kv_mx *kv, void *d_k, int64_t k_seq, i
                                int64_t v_row, int32_t out_type, int32_t n_slots, const int32_t *d_start, const int32_t *d_length, void *stream) {
     if (!kv || (!d_k && !d_v) || !d_length) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_kv_read_mx: null argument");
     KvMx c;
-    const MxRows ks = {k_seq, k_head, k_row}, vs = {v_seq, v_head, v_row};
     if (int rc = kv_mx_of(kv, &c, "bita_kv_read_mx")) return rc;
+    const MxRows ks = mx_rows(kv->batch, k_seq, kv->n_kv_heads, k_head, n_slots, k_row), vs = mx_rows(kv->batch, v_seq, kv->n_kv_heads, v_head, n_slots, v_row);
     if (int rc = check_rows("bita_kv_read_mx", out_type, n_slots, ks, vs, d_k, d_v)) return rc;
     if ((d_k && rows_overlap(kv->head_dim, {kv->batch, k_seq}, {kv->n_kv_heads, k_head}, {n_slots, k_row})) ||
         (d_v && rows_overlap(kv->head_dim, {kv->batch, v_seq}, {kv->n_kv_heads, v_head}, {n_slots, v_row})))

@@ -72,6 +72,10 @@ struct MxRows {
     int64_t seq, head, row;
     __host__ __device__ __forceinline__ int64_t at(int b, int h, int r) const { return b * seq + h * head + r * row; }
 };
+// host: strides as given, those of axes with one place (which are nobody's) as 0
+inline MxRows mx_rows(int64_t seqs, int64_t seq, int64_t heads, int64_t head, int64_t rows, int64_t row) {
+    return MxRows{seqs > 1 ? seq : 0, heads > 1 ? head : 0, rows > 1 ? row : 0};
+}
 
 // host: strides and pointers as the kernels' 16-byte accesses need them
 int mx_rows_check(const char *who, const MxRows &k, const MxRows &v, uintptr_t pointers);

@@ -104,6 +104,9 @@ extern "C" int bita_qk_norm_rope(const void *d_x, int32_t x_type, int32_t m_rows
                                  int32_t max_pos, void *d_q, int64_t ldq, int64_t q_head_stride, void *d_k, int64_t ldk, int64_t k_head_stride,
                                  void *d_v, int64_t ldv, int64_t v_head_stride, void *stream) {
     const char *who = "bita_qk_norm_rope";
+    if (m_rows <= 1) ldx = ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) * head_dim, ldq = ldk = ldv = 0;       // (strides of axes with one place are nobody's)
+    if (n_heads == 1) q_head_stride = 0;
+    if (n_kv_heads == 1) k_head_stride = v_head_stride = 0;
     if (!d_x || !d_pos || !d_cos || !d_sin || !d_q || !d_k || m_rows < 0 || n_heads <= 0 || n_kv_heads <= 0 || max_pos <= 0 || !(eps >= 0.f) || !std::isfinite(eps))
         return bita_set_error(BITA_ERR_INVALID_ARG, "%s: null argument, non-positive size or bad eps", who);
     if (x_type != BITA_F32 && x_type != BITA_BF16) return bita_set_error(BITA_ERR_INVALID_ARG, "%s: type %d", who, x_type);

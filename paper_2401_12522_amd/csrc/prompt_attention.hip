@@ -183,6 +183,9 @@ extern "C" int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_hea
     if (!d_q || !d_k || !d_v || !d_cu_seqlens || !d_out || n_seqs <= 0 || n_tokens < 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads)
         return bita_set_error(BITA_ERR_INVALID_ARG, "%s: null argument, non-positive or inconsistent size", who);
     if (head_dim != 64 && head_dim != 128) return bita_set_error(BITA_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128", who);
+    if (n_tokens <= 1) ldq = ldk = ldv = 0, ldo = (int64_t)n_heads * head_dim;                  // (strides of axes with one place are nobody's)
+    if (n_heads == 1) q_head_stride = 0;
+    if (n_kv_heads == 1) k_head_stride = v_head_stride = 0;
     if (ldq < 0 || ldk < 0 || ldv < 0 || q_head_stride < 0 || k_head_stride < 0 || v_head_stride < 0 || ldo < (int64_t)n_heads * head_dim)
         return bita_set_error(BITA_ERR_INVALID_ARG, "%s: negative stride, or output rows of %lld values %lld apart", who, (long long)n_heads * head_dim, (long long)ldo);
     if ((ldq | ldk | ldv | q_head_stride | k_head_stride | v_head_stride | ldo) & 7 ||
