@@ -65,9 +65,9 @@ __global__ __launch_bounds__(MX_THREADS) void kv_write_mx_kernel(KvMx kv, const 
                                                                  const int32_t *__restrict__ count, const int32_t *__restrict__ path, int path_stride,
                                                                  const int32_t *__restrict__ cu) {
     constexpr int PARTS = HD / 8, ROWS = MX_THREADS / PARTS;
-    const int part = threadIdx.x % PARTS, h = blockIdx.y;
-    int b = cu ? packed_sequence(cu, kv.batch, blockIdx.x * ROWS) : blockIdx.z;                // (before any lane leaves)
-    int i = blockIdx.x * ROWS + threadIdx.x / PARTS, src = i;
+    const int part = threadIdx.x % PARTS, tile = blockIdx.x / kv.Hkv, h = blockIdx.x - tile * kv.Hkv;  // (a row's heads are neighbours where rows are packed)
+    int b = cu ? packed_sequence(cu, kv.batch, tile * ROWS) : blockIdx.y;                      // (before any lane leaves)
+    int i = tile * ROWS + threadIdx.x / PARTS, src = i;
     if (i >= (path ? path_stride : n_rows)) return;
     bool ok;
     if (cu) {
@@ -184,7 +184,9 @@ extern "C" int bita_kv_write_mx(const bita_kv_mx *kv, const void *d_k, int64_t k
     if (int rc = check_rows("bita_kv_write_mx", type, n_rows, ks, vs, d_k, d_v)) return rc;
     if (n_rows == 0) return BITA_OK;
     const int per_wg = MX_THREADS * 8 / kv->head_dim;
-    const dim3 grid(((d_path ? path_stride : n_rows) + per_wg - 1) / per_wg, kv->n_kv_heads, d_cu_rows ? 1 : kv->batch);
+    const int64_t wgs = (((d_path ? path_stride : n_rows) + per_wg - 1) / per_wg) * (int64_t)kv->n_kv_heads;
+    if (wgs >= (1ll << 32) / MX_THREADS) return bita_set_error(BITA_ERR_UNSUPPORTED, "bita_kv_write_mx: %lld workgroups", (long long)wgs);
+    const dim3 grid((unsigned)wgs, d_cu_rows ? 1 : kv->batch);
 #define MX_WRITE(T_, HD_, BITS_) hipLaunchKernelGGL((kv_write_mx_kernel<T_, HD_, BITS_>), grid, dim3(MX_THREADS), 0, (hipStream_t)stream, c, (const T_ *)d_k, ks, \
                                                     (const T_ *)d_v, vs, n_rows, d_start, d_count, d_path, path_stride, d_cu_rows)
     MX_FOR(type, kv, MX_WRITE);
