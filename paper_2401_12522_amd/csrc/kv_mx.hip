@@ -66,27 +66,25 @@ __global__ __launch_bounds__(MX_THREADS) void kv_write_mx_kernel(KvMx kv, const 
                                                                  const int32_t *__restrict__ cu) {
     constexpr int PARTS = HD / 8, ROWS = MX_THREADS / PARTS;
     const int part = threadIdx.x % PARTS, tile = blockIdx.x / kv.Hkv, h = blockIdx.x - tile * kv.Hkv;  // (a row's heads are neighbours where rows are packed)
-    int b = cu ? packed_sequence(cu, kv.batch, tile * ROWS) : blockIdx.y;                      // (before any lane leaves)
-    int i = tile * ROWS + threadIdx.x / PARTS, src = i;
-    if (i >= (path ? path_stride : n_rows)) return;
-    bool ok;
+    int i = tile * ROWS + threadIdx.x / PARTS, b = cu ? 0 : blockIdx.y;
+    const int entries = path ? path_stride : n_rows, at = min(i, entries - 1);
+    const int src = min(max(path ? path[(int64_t)b * path_stride + at] : at, 0), n_rows - 1);
+    // the rows are on their way while their place is looked for
+    float x[8], y[8];
+    load8(k + ks.at(b, h, src) + part * 8, x);
+    load8(v + vs.at(b, h, src) + part * 8, y);
+    bool ok = i < entries;
     if (cu) {
+        b = packed_sequence(cu, kv.batch, tile * ROWS);
         while (b < kv.batch && cu[b + 1] <= src) b++;
-        ok = b < kv.batch;
+        ok = ok && b < kv.batch;
         b = min(b, kv.batch - 1);
         i = src - cu[b];
-        ok = ok && i >= 0 && (!count || i < count[b]);
-    } else {
-        ok = !count || i < count[b];
-        if (path) src = min(max(path[(int64_t)b * path_stride + i], 0), n_rows - 1);
     }
+    ok = ok && i >= 0 && (!count || i < count[b]);
     const int64_t slot = (int64_t)start[b] + i;
     ok = ok && slot >= 0 && slot < kv.smax;
     const int64_t row = ok ? mx_row(kv, b, h, (int)slot) : -1;
-    const int seq = cu ? 0 : b;
-    float x[8], y[8];
-    load8(k + ks.at(seq, h, src) + part * 8, x);
-    load8(v + vs.at(seq, h, src) + part * 8, y);
     put_block<HD, BITS>(x, kv.k, kv.k_scale, row, part);
     put_block<HD, BITS>(y, kv.v, kv.v_scale, row, part);
 }
