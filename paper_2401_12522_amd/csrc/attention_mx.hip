@@ -216,8 +216,8 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             const float p0 = amx_exp2(s[e] - base[u]), p1 = amx_exp2(s[e + 1] - base[u]);
-            ps += p0 + p1;
             pk[e >> 1] = amx_pk_bf16(p0, p1);
+            ps = core_add_pair(pk[e >> 1], ps);
         }
         l_run[u] += ps;
         return __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
@@ -712,7 +712,7 @@ static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int ctx_hi
             const double busy = (double)(wgs * splits) * fill;
             const double rounds = busy <= kind.slots ? 1.0 : batch > 1 ? busy / kind.slots : (double)((int64_t)(busy + kind.slots - 1) / kind.slots);
             double us = kind.start + rounds * (double)turns * size * (busy <= 256 ? kind.one : kind.many);
-            if (splits > 1) us += 2.5 + 0.03 * (double)splits + (double)(queries * splits) * fill * hd * 8 / 4.5e6;
+            if (splits > 1) us += 3.5 + 0.03 * (double)splits + (double)(queries * splits) * fill * hd * 8 / 4.5e6;
             if (us < best) {
                 best = us;
                 p.wide = k == 3;

@@ -57,7 +57,8 @@ def rounded(v, bits):
 def attention(q, k, v, seen):
     """q [n][hd], k, v [m][hd], seen [n][m], float64: the weighted means (zeros for a row that sees nothing) and how far a
     kernel that rounds the probabilities and the result to bf16 and computes in fp32 may be off, element by element:
-      probabilities: half a step of bf16, and the error e of their exponents on all of them and on their sum;
+      probabilities: half a step of bf16, and the error e of their exponents, on all of them and on their sum (which may be taken
+      before or after the rounding);
       e: a dot product of hd terms in fp32, its scaling, the exponential (1 unit in 2^22), next to scores of size s;
       sums over m terms in fp32; the result: half a step of bf16;
       fp32 ends at 2^-126: a probability (relative to the largest, which is 1, so the sum is at least 1), a share's weight or a
@@ -74,6 +75,6 @@ def attention(q, k, v, seen):
     o = p @ vz
     unit = 2.0 ** -24
     e = (hd + 4) * unit * size + 3 * unit * size + 2.0 ** -22
-    off = (HALF_BF16 + 2 * e + 2 * k.shape[0] * unit) * (p @ vz.abs())
+    off = (2 * HALF_BF16 + 2 * e + 2 * k.shape[0] * unit) * (p @ vz.abs())
     off = off + 3 * 2.0 ** -126 * (vz.abs() + 1).sum(0)
     return o, off + HALF_BF16 * (o.abs() + off)
