@@ -9,18 +9,20 @@
 #define MX_THREADS 256
 #define MX_MAX_ROWS (1 << 27)           // of a call and sequence: a grid holds 2^32 threads along x
 
-// One row's place: the sequence and number of the row among the sequence's, from a row of the packed axis.
-// The first sequence is found by all lanes at once (64 starts a step), a thread's own by walking on from it.
+// The sequence of a row of the packed axis: the last one that starts at or before it (`batch`: the row is behind all of them; 0 also where it is before
+// all).  64 starts are looked at in a step, and the 64th part they leave in the next.
 __device__ __forceinline__ int packed_sequence(const int32_t *__restrict__ cu, int batch, int row) {
     const int lane = threadIdx.x & 63;
-    int b = 0;
-    for (int j0 = 0; j0 <= batch; j0 += 64) {
-        const bool at_or_before = j0 + lane <= batch && cu[min(j0 + lane, batch)] <= row;
-        const uint64_t m = __builtin_amdgcn_ballot_w64(at_or_before);
-        if (m == 0) break;
-        b = j0 + 63 - __builtin_clzll(m);
+    int b = 0, n = batch + 1;                                   // it is among n from b on
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lane * step;
+        const uint64_t before = __builtin_amdgcn_ballot_w64(at < n && cu[b + min(at, n - 1)] <= row);
+        if (before == 0) break;
+        const int last = 63 - __builtin_clzll(before);
+        b += last * step;
+        n = min(step, n - last * step);
     }
-    return b;                                                   // (the last one that starts at or before the row; batch: the end does)
+    return b;
 }
 
 template <typename T>

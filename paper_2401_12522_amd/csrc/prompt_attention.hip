@@ -15,6 +15,7 @@
 
 #define PA_WAVES 4
 #define PA_ROWS (32 * PA_WAVES)
+#define PA_SKIP 8
 #define PA_MAX_LD (1 << 24)            // offsets inside a tile of 64 rows have 32 bits (signed)
 
 struct PromptArgs {
@@ -30,14 +31,28 @@ struct PromptArgs {
 // down, over 64 sequences (a lane each) at a time: of every number the tiles that sequences have, until `tile` is reached.  false: no such tile.
 __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &start, int &len, int &mine) {
     const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-        const int b = b0 + lane;
-        int s = 0, n = 0;
+    auto sequence = [&](int b, int &s, int &n) __attribute__((always_inline)) {
+        s = n = 0;
         if (b < a.n_seqs) {
             s = min(max(a.cu[b], 0), a.n_tokens);
             n = min(max(a.cu[b + 1], s), a.n_tokens) - s;
         }
-        const int tiles = (n + PA_ROWS - 1) / PA_ROWS;
+        return (n + PA_ROWS - 1) / PA_ROWS;
+    };
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+        while (a.n_seqs - b0 > PA_SKIP * 64) {                                          // (of very many, 8 a lane are passed over at a time)
+            int s, n, all = 0;
+#pragma unroll
+            for (int i = 0; i < PA_SKIP; i++) all += sequence(b0 + 64 * i + lane, s, n);
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
+            all = __builtin_amdgcn_readfirstlane(all);
+            if (tile < all) break;
+            tile -= all;
+            b0 += PA_SKIP * 64;
+        }
+        int s, n;
+        const int tiles = sequence(b0 + lane, s, n);
         int all = tiles, most = tiles;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {

@@ -148,6 +148,24 @@ def test_packed_rows(bits, hd, page, dtype):
     check(cache, k, v, n, start, lens)
 
 
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 4097, 5000])
+def test_packed_rows_of_very_many_sequences(n):
+    import paper_2401_12522_amd as bita
+    lens = [(i * 5) % 3 for i in range(n)]
+    cu = [3]                                                     # (rows before the first sequence are nobody's)
+    for x in lens:
+        cu.append(cu[-1] + x)
+    k = rows((cu[-1] + 2, 1, 64), n)
+    cache = make(1, 64, n, 3, 4)
+    bita.kv_write_mx(cache, k.cuda(), k.cuda(), i32([0] * n), cu_rows=i32(cu))
+    c, s = ref.quantize(k, 4)
+    c = ref.pack(c, 4)
+    want_c, want_s = torch.zeros(n, 3, 32, dtype=torch.uint8), torch.full((n, 3, 2), 127, dtype=torch.uint8)
+    for b in range(n):
+        want_c[b, : lens[b]], want_s[b, : lens[b]] = c[cu[b]: cu[b + 1], 0], s[cu[b]: cu[b + 1], 0]
+    assert torch.equal(cache.k.cpu()[:, 0], want_c) and torch.equal(cache.v_scale.cpu()[:, 0], want_s)
+
+
 @BITS
 def test_accepted_rows_by_their_path(bits):
     import paper_2401_12522_amd as bita

@@ -56,6 +56,19 @@ def test_against_float64(lens, hq, hkv, hd, fused):
     assert (got[cu[-1]:] == 5).all()
 
 
+@pytest.mark.parametrize("n", [64, 65, 513, 1100, 3000])
+def test_very_many_short_sequences(n):
+    """Against the same sequences one call each would give: lengths 0 to 3 and a few of some hundred rows among them."""
+    import paper_2401_12522_amd as bita
+    lens = [(i * 7) % 4 for i in range(n)]
+    for i in (0, n // 2, n - 1):
+        lens[i] = 150 + i % 100
+    cu = starts(lens)
+    q, k, v = tensors(cu[-1], 2, 1, 64)
+    out, tol = expected(q, k, v, cu)
+    near(bita.prompt_attention(q.cuda(), k.cuda(), v.cuda(), i32(cu)), out, tol)
+
+
 def test_rows_before_the_first_sequence_and_wide_output_rows():
     import paper_2401_12522_amd as bita
     q, k, v = tensors(60, 4, 2, 64)
