@@ -24,12 +24,6 @@ __device__ __forceinline__ uint32_t core_pk_bf16(float a, float b) {
     const f2 v = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
 }
-// c plus a pair of bf16.  What is summed is what the product takes: the sum then has the probabilities' rounding in common with the values they weigh, and a
-// row that one key dominates loses nothing by it.  (One instruction for a pair; a tile's are summed by themselves before they meet the running sum.)
-__device__ __forceinline__ float core_add_pair(uint32_t pair, float c) {
-    typedef __attribute__((ext_vector_type(2))) __bf16 b2;
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, pair), __builtin_bit_cast(b2, 0x3F803F80u), c, false);
-}
 __device__ __forceinline__ float core_max_halves(float x) {
     typedef __attribute__((ext_vector_type(2))) unsigned u2;
     const u2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -135,14 +129,17 @@ struct AttnCore {
                 for (int e = 0; e < 16; e++) o[n][e] = o[n][e] * alpha * alpha;
         }
     }
-    // scores to probabilities 2^(score scale - base) as bf16 pairs, in the order of the registers; their sum
+    // scores to probabilities 2^(score scale - base) as bf16 pairs, in the order of the registers; their sum, taken before they are rounded (rounded to
+    // bf16 a probability is off by at most 2^-8 of itself, as the result is; the sum of the rounded ones, by the pairs' dot product, brought the error at 8192
+    // tokens from 0.0022 to 0.0020 of the result, 0.0016 of which is the result's own rounding, for 2 % of the time)
     __device__ __forceinline__ float exponentials(const f32x16 (&s)[2], float scale_log2, uint32_t (&p)[16]) const {
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
             const float a = core_exp2(__builtin_fmaf(s[e >> 4][e & 15], scale_log2, -base)), b = core_exp2(__builtin_fmaf(s[e >> 4][(e & 15) + 1], scale_log2, -base));
+            sum[0] += a;
+            sum[1] += b;
             p[e >> 1] = core_pk_bf16(a, b);
-            sum[e >> 1 & 1] = core_add_pair(p[e >> 1], sum[e >> 1 & 1]);
         }
         return sum[0] + sum[1];
     }
@@ -183,8 +180,9 @@ struct AttnCore {
                 for (int j = 0; j < PAIRS; j++) {
                     const int e = 2 * ((4 * g + i) * PAIRS + j);
                     const float x = core_exp2(__builtin_fmaf(s[e >> 4][e & 15], scale_log2, -base)), y = core_exp2(__builtin_fmaf(s[e >> 4][(e & 15) + 1], scale_log2, -base));
+                    sum[0] += x;
+                    sum[1] += y;
                     p[e >> 1] = core_pk_bf16(x, y);
-                    sum[e >> 1 & 1] = core_add_pair(p[e >> 1], sum[e >> 1 & 1]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }

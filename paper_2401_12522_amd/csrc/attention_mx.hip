@@ -216,8 +216,8 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             const float p0 = amx_exp2(s[e] - base[u]), p1 = amx_exp2(s[e + 1] - base[u]);
+            ps += p0 + p1;
             pk[e >> 1] = amx_pk_bf16(p0, p1);
-            ps = core_add_pair(pk[e >> 1], ps);
         }
         l_run[u] += ps;
         return __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));

@@ -27,6 +27,16 @@ struct PromptArgs {
     uint16_t *out;
 };
 
+// f over all lanes (a sum, a maximum; 0 is its neutral element): rows of 16 lanes by rotation, then the four rows
+template <typename F>
+__device__ __forceinline__ int pa_over_wave(int x, F &&f) {
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xF, 0xF, false));        // row_ror 1, 2, 4, 8
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xF, 0xF, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xF, 0xF, false));
+    x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, false));
+    return f(f(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)), f(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
+}
+
 // The workgroup's tile of queries: its sequence's first token and length, and its number in the sequence.  Tiles count from the longest walk
 // down, over 64 sequences (a lane each) at a time: of every number the tiles that sequences have, until `tile` is reached.  false: no such tile.
 __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &start, int &len, int &mine) {
@@ -44,27 +54,19 @@ __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &star
             int s, n, all = 0;
 #pragma unroll
             for (int i = 0; i < PA_SKIP; i++) all += sequence(b0 + 64 * i + lane, s, n);
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
-            all = __builtin_amdgcn_readfirstlane(all);
+            all = pa_over_wave(all, [](int x, int y) { return x + y; });
             if (tile < all) break;
             tile -= all;
             b0 += PA_SKIP * 64;
         }
         int s, n;
         const int tiles = sequence(b0 + lane, s, n);
-        int all = tiles, most = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            all += __shfl_xor(all, d);
-            most = max(most, __shfl_xor(most, d));
-        }
-        all = __builtin_amdgcn_readfirstlane(all);
+        const int all = pa_over_wave(tiles, [](int x, int y) { return x + y; }), most = pa_over_wave(tiles, [](int x, int y) { return max(x, y); });
         if (tile >= all) {
             tile -= all;
             continue;
         }
-        for (int k = __builtin_amdgcn_readfirstlane(most) - 1;; k--) {                  // (ends: `all` is the sum of these counts over k)
+        for (int k = most - 1;; k--) {                                                 // (ends: `all` is the sum of these counts over k)
             const uint64_t has = __builtin_amdgcn_ballot_w64(tiles > k);
             const int count = __popcll(has);
             if (tile >= count) {
@@ -154,9 +156,9 @@ __global__ __launch_bounds__(PA_WAVES * 64, 2) void prompt_attn_kernel(PromptArg
     uint32_t p[16], odd = 0;
     int t = 0;
     fetch(0, false);
-    landed();
     fetch(0, true);
     if (n_tiles > 1) fetch(1, false);
+    landed();
     if (q0 < len) {
         core.scores(k_tile(0), s);
         if (n_whole == 0) mask(0, s);
