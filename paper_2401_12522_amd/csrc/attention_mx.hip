@@ -12,6 +12,7 @@
 //    B operand of O^T = V^T P^T if that product takes the keys in the same order: probabilities stay in registers.
 //  * V^T needs eight keys of one column in a lane: V goes to LDS as bf16 rows and comes back by transposed reads.  The region is the wave's own,
 //    and its LDS instructions run in order, so there is no barrier in the loop.
+#include <algorithm>
 #include <cmath>
 #include "mx.h"
 #include "attention_core.h"
@@ -684,23 +685,27 @@ static void launch_merge(const AmxArgs &a, int64_t queries, int n_splits, hipStr
 
 struct AmxPlan { bool wide; int tiles_u, waves, n_tiles, splits, per_split; int64_t workgroups; size_t part_o, part_ml; };
 
-// How a launch is cut, from nothing but its sizes: one tile of 16 queries a workgroup, two, or 128 queries that share decoded keys (wide); and the keys into
+// How a launch is cut, from nothing but its sizes: 16 queries a workgroup of 8 waves or of 4, 32 queries, or 128 that share decoded keys (wide); and the keys into
 // shares, which go by the hint, so that shorter sequences of a batch have fewer of them.  The estimate behind the choice, in us at head_dim 128:
-//   a workgroup's start and end, its turns (128 keys, wide 64) at the pace of one workgroup a CU or of as many as a CU holds, and,
-//   where the keys are split, a second kernel and what the shares write and read, at 4.5 TB/s.
-// Measured (one / two tiles / wide): a turn with one workgroup a CU 0.9 / 1.25 / 1.56, with two 1.44 / 2.1 / 2.43; the start and end 5.6 / 5.6 / 7.  The batch's
-// lengths are taken to be three quarters of the hint on average.  32 sequences of up to 8192 keys, 64/8 heads, shares of 4096, 2048, 1365, 1024 keys
-// 45.1, 35.0, 39.1, 38.8 us; 4 sequences of 1024 to 4096, 68 rows (wide) in 2, 3, 4, 5 shares 69.4, 64.7, 58.5, 66.8, in tiles of 32 queries 76;
-// one of 131072 in 47, 61, 79, 94 shares 39.1, 33.5, 36.1, 35.0; one of 1000, 32 heads, in 1, 2, 3, 5, 9 shares 13.6, 11.5, 10.1, 8.8, 8.7.
-static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int ctx_hint, int n_prompt) {
+//   a round of workgroups: their start and end, and their turns (256 keys, 128, 128, 64) at the pace of one workgroup a CU or of as many as a CU holds, but no faster
+//   than a CU takes codes in, 35 KB a us; the bytes that all of them read at 6 TB/s, 5 where tiles of queries read the same ones again (of these two the longer, and a
+//   quarter of the other); and, where the keys are split, a second kernel and what the shares write and read, at 4.5 TB/s.
+// Measured (16 queries in 4 waves / 32 / wide): a turn with one workgroup a CU 0.9 / 1.25 / 1.56 us, with two 1.44 / 2.1 / 2.43; the start and end 5.6 / 5.6 / 7; a turn of
+// 8 waves 1.0.  A batch's lengths are taken to be half to three quarters of the hint on average.  Each kind with its best shares, 16 queries in 8 waves / in 4 / 32 / wide:
+//   68 rows, 32 heads of their own keys, 1024 keys of 4 bits 11.8 / 14.2 / 16.1 / 19.1 us; 4096 keys of 8 bits 41.8 / 40.7 / 28.4 / 24.1; four sequences of 400 to 1100
+//   keys 31.2 / 21.6 / 30.3 / 28.5; 4 sequences of 1024 to 4096 keys, 64/8 heads 145 / 127 / 81 / 57; 20 rows there 38.4 / 34.5 / 30.5 / 40.4; single tokens: 32 sequences
+//   of up to 8192 keys 42.8 / 35.7 / 47 / 82; one of 131072 keys of 4 bits 31.2 / 36.6 / 41.2 / 59; one of 1000, 32 heads 10.2 / 9.3 / 9.7 / 11.3 (the last three with
+//   a second kernel, whose launch costs the host as much again: hence 3.5 us for it, more than its own time).
+static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int bits, int ctx_hint, int n_prompt) {
     static const struct { int queries, unit, waves, slots; double start, one, many; } kinds[4] = {
         {16, AMX_CHUNK, 8, 256, 5.6, 1.0, 1.0}, {16, AMX_CHUNK, 4, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, 4, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 4, 512, 7.0, 1.56, 2.43}};
     static const int shares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128, 192, 256};
     const int64_t nq = (int64_t)rows * (Hq / Hkv), queries = (int64_t)batch * rows * Hq;
     const double fill = batch > 1 ? 0.75 : 1.0, size = hd / 128.0;
+    const double key_bytes = 2 * (hd * bits / 8 + hd / 32), cache = (double)batch * Hkv * ctx_hint * (batch > 1 ? 0.5 : 1.0) * key_bytes;
     AmxPlan p = {};
     double best = 1e300;
-    for (int k = nq <= 16 ? 0 : 2; k < (nq <= 16 ? 2 : nq <= 32 ? 3 : 4); k++) {
+    for (int k = 0; k < (nq <= 16 ? 2 : nq <= 32 ? 3 : 4); k++) {
         const auto &kind = kinds[k];
         const int unroll = k == 3 ? 1 : kind.waves;                             // chunks of a turn
         const int n_tiles = (int)((nq + kind.queries - 1) / kind.queries);
@@ -709,9 +714,12 @@ static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int ctx_hi
         for (int want : shares) {
             if (want > 1 && want * unroll > chunks) break;
             const int64_t turns = (chunks + (int64_t)want * unroll - 1) / ((int64_t)want * unroll), per = turns * unroll, splits = (chunks + per - 1) / per;
-            const double busy = (double)(wgs * splits) * fill;
-            const double rounds = busy <= kind.slots ? 1.0 : batch > 1 ? busy / kind.slots : (double)((int64_t)(busy + kind.slots - 1) / kind.slots);
-            double us = kind.start + rounds * (double)turns * size * (busy <= 256 ? kind.one : kind.many);
+            const double busy = (double)(wgs * splits) * (k ? fill : 1.0);         // (alone on a CU, a short workgroup leaves it to the next one late)
+            const double rounds = k && batch > 1 ? std::max(busy / kind.slots, 1.0) : (double)((wgs * splits + kind.slots - 1) / kind.slots);
+            const double on_a_cu = std::min(busy < 256 ? 1.0 : busy / 256, kind.slots / 256.0);
+            const double turn = std::max(size * (busy <= 256 ? kind.one : kind.many), on_a_cu * unroll * kind.unit * key_bytes / 35e3);
+            const double pace = rounds * (double)turns * turn, load = cache * n_tiles / (n_tiles > 1 ? 5e6 : 6e6);
+            double us = rounds * kind.start + std::max(pace, load) + 0.25 * std::min(pace, load);
             if (splits > 1) us += 3.5 + 0.03 * (double)splits + (double)(queries * splits) * fill * hd * 8 / 4.5e6;
             if (us < best) {
                 best = us;
@@ -742,7 +750,7 @@ static int amx_sizes(const char *who, int32_t batch, int32_t rows, int32_t n_hea
 extern "C" size_t bita_tree_attention_mx_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t bits,
                                                          int32_t ctx_hint, int32_t n_prompt) {
     if (amx_sizes("bita_tree_attention_mx_workspace_bytes", batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt)) return 0;
-    const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, ctx_hint, n_prompt);
+    const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt);
     return p.part_o + p.part_ml;
 }
 
@@ -750,7 +758,7 @@ extern "C" int bita_tree_attention_mx_plan_info(int32_t batch, int32_t rows, int
                                                 int32_t n_prompt, int32_t *out4) {
     if (!out4) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_tree_attention_mx_plan_info: null argument");
     if (int rc = amx_sizes("bita_tree_attention_mx_plan_info", batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt)) return rc;
-    const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, ctx_hint, n_prompt);
+    const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt);
     out4[0] = p.splits; out4[1] = p.wide ? AMW_ROWS : 16 * p.tiles_u; out4[2] = p.waves;
     out4[3] = p.workgroups < INT32_MAX ? (int32_t)p.workgroups : INT32_MAX;
     return BITA_OK;
@@ -785,7 +793,7 @@ extern "C" int bita_tree_attention_mx(const bita_tree_template *t, const void *d
     a.v_at = mx_rows(kv->batch, v_seq, kv->n_kv_heads, v_head, t->dev.rows, v_row);
     if (int rc = mx_rows_check(who, a.k_at, a.v_at, (uintptr_t)d_q | (uintptr_t)d_k_rows | (uintptr_t)d_v_rows | (uintptr_t)d_prompt_k | (uintptr_t)d_prompt_v |
                                                         (uintptr_t)d_out | (uintptr_t)d_ws)) return rc;
-    const AmxPlan p = amx_plan(kv->batch, t->dev.rows, n_heads, kv->n_kv_heads, kv->head_dim, ctx_hint, n_prompt);
+    const AmxPlan p = amx_plan(kv->batch, t->dev.rows, n_heads, kv->n_kv_heads, kv->head_dim, kv->bits, ctx_hint, n_prompt);
     if (ws_bytes < p.part_o + p.part_ml || (p.splits > 1 && !d_ws))
         return bita_set_error(BITA_ERR_CAPACITY, "%s: workspace %zu < %zu bytes", who, ws_bytes, p.part_o + p.part_ml);
     a.t = t->dev;

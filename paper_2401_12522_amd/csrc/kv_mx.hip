@@ -174,7 +174,7 @@ int mx_rows_check(const char *who, const MxRows &k, const MxRows &v, uintptr_t p
 extern "C" int bita_kv_write_mx(const bita_kv_mx *kv, const void *d_k, int64_t k_seq, int64_t k_head, int64_t k_row, const void *d_v, int64_t v_seq,
                                 int64_t v_head, int64_t v_row, int32_t type, int32_t n_rows, const int32_t *d_start, const int32_t *d_count, const int32_t *d_path,
                                 int32_t path_stride, const int32_t *d_cu_rows, void *stream) {
-    if (!kv || !d_k || !d_v || !d_start) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_kv_write_mx: null argument");
+    if (!kv || (n_rows && (!d_k || !d_v)) || !d_start) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_kv_write_mx: null argument");
     if (d_path && (d_cu_rows || path_stride <= 0 || path_stride > MX_MAX_ROWS))
         return bita_set_error(BITA_ERR_INVALID_ARG, "bita_kv_write_mx: a path has a positive length and goes with rows by sequence");
     KvMx c;
@@ -196,7 +196,7 @@ extern "C" int bita_kv_write_mx(const bita_kv_mx *kv, const void *d_k, int64_t k
 
 extern "C" int bita_kv_read_mx(const bita_kv_mx *kv, void *d_k, int64_t k_seq, int64_t k_head, int64_t k_row, void *d_v, int64_t v_seq, int64_t v_head,
                                int64_t v_row, int32_t out_type, int32_t n_slots, const int32_t *d_start, const int32_t *d_length, void *stream) {
-    if (!kv || (!d_k && !d_v) || !d_length) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_kv_read_mx: null argument");
+    if (!kv || (n_slots && !d_k && !d_v) || !d_length) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_kv_read_mx: null argument");
     KvMx c;
     if (int rc = kv_mx_of(kv, &c, "bita_kv_read_mx")) return rc;
     const MxRows ks = mx_rows(kv->batch, k_seq, kv->n_kv_heads, k_head, n_slots, k_row), vs = mx_rows(kv->batch, v_seq, kv->n_kv_heads, v_head, n_slots, v_row);

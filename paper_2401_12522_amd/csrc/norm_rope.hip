@@ -129,7 +129,7 @@ extern "C" int bita_qk_norm_rope(const void *d_x, int32_t x_type, int32_t m_rows
     if (m_rows <= 1) ldx = ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) * head_dim, ldq = ldk = ldv = 0;       // (strides of axes with one place are nobody's)
     if (n_heads == 1) q_head_stride = 0;
     if (n_kv_heads == 1) k_head_stride = v_head_stride = 0;
-    if (!d_x || !d_pos || !d_cos || !d_sin || !d_q || !d_k || m_rows < 0 || n_heads <= 0 || n_kv_heads <= 0 || max_pos <= 0 || !(eps >= 0.f) || !std::isfinite(eps))
+    if ((m_rows && (!d_x || !d_pos || !d_q || !d_k)) || !d_cos || !d_sin || m_rows < 0 || n_heads <= 0 || n_kv_heads <= 0 || max_pos <= 0 || !(eps >= 0.f) || !std::isfinite(eps))
         return bita_set_error(BITA_ERR_INVALID_ARG, "%s: null argument, non-positive size or bad eps", who);
     if (x_type != BITA_F32 && x_type != BITA_BF16) return bita_set_error(BITA_ERR_INVALID_ARG, "%s: type %d", who, x_type);
     const int64_t heads = (int64_t)n_heads + 2 * (int64_t)n_kv_heads;

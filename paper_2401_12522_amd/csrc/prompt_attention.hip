@@ -197,7 +197,7 @@ extern "C" int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_hea
                                      const void *d_v, int64_t ldv, int64_t v_head_stride, const int32_t *d_cu_seqlens, int32_t n_seqs, int32_t n_tokens,
                                      int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void *d_out, int64_t ldo, void *stream) {
     const char *who = "bita_prompt_attention";
-    if (!d_q || !d_k || !d_v || !d_cu_seqlens || !d_out || n_seqs <= 0 || n_tokens < 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads)
+    if ((n_tokens && (!d_q || !d_k || !d_v || !d_out)) || !d_cu_seqlens || n_seqs <= 0 || n_tokens < 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads)
         return bita_set_error(BITA_ERR_INVALID_ARG, "%s: null argument, non-positive or inconsistent size", who);
     if (head_dim != 64 && head_dim != 128) return bita_set_error(BITA_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128", who);
     if (n_tokens <= 1) ldq = ldk = ldv = 0, ldo = (int64_t)n_heads * head_dim;                  // (strides of axes with one place are nobody's)

@@ -258,3 +258,28 @@ def test_same_result_every_time_eager_and_replayed(bits):
         torch.cuda.synchronize()
         for (o, _), w in zip(outs, want):
             assert torch.equal(o, w)
+
+
+@BITS
+@pytest.mark.parametrize("cut,n,R,masks,hq,hkv,hd,ctx,page,P", [
+    ((16, 4, False), 2, 20, 4, 2, 2, 64, [40, 33], 16, 5),
+    ((16, 8, False), 1, 35, 3, 4, 4, 128, [300], 64, 16),       # three tiles a head that read the same keys
+    ((16, 8, True), 1, 33, 0, 2, 1, 64, [6000], 0, 40),
+    ((32, 4, False), 8, 20, 2, 32, 16, 64, [40, 39, 31, 0, 1, 33, 32, 17], 32, 3),
+    ((32, 4, True), 17, 5, 2, 8, 2, 128, [1500, 0, 1, 700, 64, 32, 33, 31, 900, 1499, 10, 128, 127, 129, 300, 256, 255], 64, 40),
+    ((128, 4, False), 17, 68, 4, 64, 2, 64, [40, 39, 31, 0, 1, 33, 32, 17, 40, 5, 6, 7, 8, 9, 10, 11, 12], 16, 3),
+    ((128, 4, True), 1, 130, 5, 16, 1, 128, [6000], 256, 16),
+])
+def test_every_cut_of_a_launch(bits, cut, n, R, masks, hq, hkv, hd, ctx, page, P):
+    """The kinds of workgroups, with one share of the keys and with several, and a NaN among the pass' values, which reaches the rows that see it only."""
+    import paper_2401_12522_amd as bita
+    plan = bita.binding.tree_attention_mx_plan_info(n, R, hq, hkv, hd, bits, max(ctx), P)
+    assert (plan["queries"], plan["waves"], plan["splits"] > 1) == cut
+    call, (out, tol), (cache, q, kr, vr, _, _, tmpl, seen, _) = case(n, R, masks, hq, hkv, hd, bits, ctx, page, P, seed=7)
+    near(call(), out, tol)
+    at = R - masks - 1
+    vr[:, :, at, 3] = float("nan")
+    got = call().cpu().double().view(out.shape)
+    assert torch.isnan(got[:, seen[:, at]][..., 3]).all()
+    got[..., 3] = torch.where(seen[:, at][None, :, None], out[..., 3], got[..., 3])
+    near(got, out, tol)
