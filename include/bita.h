@@ -417,7 +417,8 @@ typedef struct bita_kv_mx {
  *             rows outside all of them are left out
  * bita_kv_read_mx is the way back: slot d_start[b] + i, i < min(d_length[b], n_slots), of head h to out_type values at
  * b * seq + h * head + i * row of d_k and d_v (either may be NULL); slots outside 0 .. smax-1 and everything
- * behind a sequence's length are left as they are.  d_start NULL: 0.  Neither changes a length.  One kernel each; may be captured. */
+ * behind a sequence's length are left as they are.  d_start NULL: 0.  Neither changes a length.  n_rows, n_slots and path_stride at most 2^27; a
+ * stride of an axis with one place is not looked at; rows of an output do not overlap.  No rows: the row pointers may be NULL.  One kernel each; may be captured. */
 int bita_kv_write_mx(const bita_kv_mx *kv, const void *d_k, int64_t k_seq, int64_t k_head, int64_t k_row, const void *d_v, int64_t v_seq, int64_t v_head,
                      int64_t v_row, int32_t type, int32_t n_rows, const int32_t *d_start, const int32_t *d_count, const int32_t *d_path, int32_t path_stride,
                      const int32_t *d_cu_rows, void *stream);
@@ -441,14 +442,16 @@ int bita_qk_norm_rope(const void *d_x, int32_t x_type, int32_t m_rows, int64_t l
  *   d_k_rows, d_v_rows  bf16, of head h, row r of sequence b the hd values at b * seq + h * head + r * row (strides k_* and v_* in
  *          elements, multiples of 8): the rows' K/V, not yet in the cache
  *   d_prompt_k, d_prompt_v  bf16 [n_kv_heads][n_prompt][hd] or NULL with n_prompt 0
- *   d_ctx_len [B] (read as at most ctx_hint and smax);  ctx_hint: HOST upper bound of them, at most smax
+ *   d_ctx_len [B] (read as at most ctx_hint and smax);  ctx_hint: HOST upper bound of them, at most smax (2^30).  It decides the launch and the
+ *          workspace; which keys a workgroup takes follows from the lengths themselves (up to 64 sequences), so that a graph captured for long
+ *          sequences keeps the card busy over short ones
  *   d_token   [B][R] or NULL: a tree row with a negative token is absent and its output zero (it stays visible to the rows below it)
  *   d_out  bf16 [B][R][n_heads * hd];  d_ws: bita_tree_attention_mx_workspace_bytes(), a multiple of 16, nothing in it kept from call to call, calls that
  *          may run at the same time have each their own.  The pointers of bf16 tensors are multiples of 16 bytes.
- * Any n_heads that is a multiple of n_kv_heads.  One kernel, or two where the keys are split; may be captured.  Scores, sums and
+ * Any n_heads that is a multiple of n_kv_heads; batch * n_heads at most 2^17, n_prompt at most 2^20.  One kernel, or two where the keys are split; may be captured.  Scores, sums and
  * accumulation are fp32; probabilities go to the matrix product as bf16.
- * bita_tree_attention_mx_plan_info: how it is cut (for tests and reports): out4 (HOST) = {key splits, queries of a workgroup, waves of a
- * workgroup, workgroups}. */
+ * bita_tree_attention_mx_plan_info: how it is cut (for tests and reports): out4 (HOST) = {shares that a sequence's keys are
+ * split into, on average and rounded up, queries of a workgroup, waves of a workgroup, workgroups}. */
 size_t bita_tree_attention_mx_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t bits,
                                               int32_t ctx_hint, int32_t n_prompt);
 int bita_tree_attention_mx_plan_info(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t bits, int32_t ctx_hint,
@@ -464,8 +467,8 @@ int bita_tree_attention_mx(const bita_tree_template *t, const void *d_q, const b
  *                  their own, or columns of one QKV product
  *   d_cu_seqlens   [n_seqs + 1], device, not decreasing, between 0 and n_tokens (clamped; sequences may be empty)
  *   d_out          bf16 rows of n_heads * head_dim, ldo apart; rows outside all sequences are left as they are
- * head_dim 64 or 128, any n_heads that is a multiple of n_kv_heads.  Scores, sums and accumulation are fp32; probabilities go to the matrix
- * product as bf16.  One kernel; may be captured. */
+ * head_dim 64 or 128, any n_heads that is a multiple of n_kv_heads; rows of k and of v at most 2^24 elements apart.  Scores, sums and accumulation
+ * are fp32; probabilities go to the matrix product as bf16.  One kernel; may be captured. */
 int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_head_stride, const void *d_k, int64_t ldk, int64_t k_head_stride, const void *d_v,
                           int64_t ldv, int64_t v_head_stride, const int32_t *d_cu_seqlens, int32_t n_seqs, int32_t n_tokens, int32_t n_heads,
                           int32_t n_kv_heads, int32_t head_dim, void *d_out, int64_t ldo, void *stream);

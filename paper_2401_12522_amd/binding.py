@@ -882,7 +882,7 @@ def _attention_mx_scratch(*sizes):
 
 
 def tree_attention_mx_plan_info(batch, rows, heads, kv_heads, head_dim, bits, ctx_hint, n_prompt=0):
-    """{splits (of the keys), queries, waves (of a workgroup), workgroups} that tree_attention_mx of these sizes launches."""
+    """{splits (of a sequence's keys, on average), queries, waves (of a workgroup), workgroups} that tree_attention_mx of these sizes launches."""
     out = (C.c_int32 * 4)()
     _check(lib().bita_tree_attention_mx_plan_info(batch, rows, heads, kv_heads, head_dim, bits, int(ctx_hint), n_prompt, out))
     return dict(splits=out[0], queries=out[1], waves=out[2], workgroups=out[3])

@@ -4,7 +4,7 @@
 // A K/V head's queries are one axis: R rows times the heads of its group, 16 of them a tile, whatever the number of heads.  A workgroup
 // owns U tiles and a share of the keys, which its waves walk in chunks of 32, each with its own running maximum and sum; the waves' results meet
 // in LDS once at the end, the shares' (where the keys are split over workgroups) in a second kernel.
-//  * Codes go from memory to registers, a chunk ahead of the arithmetic, and from there to bf16 (exact: a code times a power of two) by
+//  * Codes go from memory to registers, two chunks ahead of the arithmetic (one with two tiles), and from there to bf16 (exact: a code times a power of two) by
 //    conversion instructions that apply the scale: a lane holds a quarter of a key's head, one block of 32 values (half of one at 64).
 //  * The contraction over the head runs in the order in which a lane holds it: k-step s takes values 8s .. 8s+7 of every lane's
 //    quarter, of the queries too, so K needs no other layout than the cache's.
@@ -12,7 +12,10 @@
 //    B operand of O^T = V^T P^T if that product takes the keys in the same order: probabilities stay in registers.
 //  * V^T needs eight keys of one column in a lane: V goes to LDS as bf16 rows and comes back by transposed reads.  The region is the wave's own,
 //    and its LDS instructions run in order, so there is no barrier in the loop.
+// Bound by what a CU takes in at low batch (one sequence of 131072 keys, 64/8 heads, 4 bits: 143 MB in 28 us, 5.1 TB/s, and a merge of 4), by its own start and end at
+// short lengths (1000 keys, 32 heads: 10 us for 4.4 MB), by the conversions and the exponentials between, where a K/V head has many queries by matrix instructions.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include "mx.h"
 #include "attention_core.h"
@@ -41,24 +44,100 @@ struct AmxArgs {
     const uint16_t *q, *k_rows, *v_rows, *prompt_k, *prompt_v;
     MxRows k_at, v_at;
     const int32_t *ctx_len, *token;
-    int P, R, qpk, ctx_hint, n_tiles, n_splits, per_split;      // tiles of a workgroup's queries, shares of the keys, chunks (tiles) of a share
+    int P, R, qpk, ctx_hint, n_tiles, n_shares, per_share;      // tiles of a workgroup's queries; shares of all sequences' keys together (as many: nothing is split); turns of a share where the batch is large
     float scale_log2;
-    float *part_o, *part_ml;
+    float *part_o, *part_ml;                                    // [share][R * heads][HD], [..][2]
+    int2 *share_of;                                             // [batch]: a sequence's first share and how many it has
     uint16_t *out;
+    __device__ __forceinline__ int length(int b) const { return min(max(ctx_len[b], 0), min(ctx_hint, kv.smax)); }
+    // of a query (row, head) of sequence b: where it is in out and q, and where in a share's part
+    __device__ __forceinline__ int64_t query(int b, int row, int head) const { return ((int64_t)b * R + row) * (qpk * kv.Hkv) + head; }
+    __device__ __forceinline__ int64_t part(int share, int row, int head) const { return ((int64_t)share * R + row) * (qpk * kv.Hkv) + head; }
 };
 
-// Workgroup id -> (tile of queries, share of the keys, sequence, K/V head).  The tiles that read the same keys go to one XCD, one behind the other: ids go round
-// over the 8 XCDs, and the shares with them, a head's neighbours first.  (Quotients are worked out in vector registers: without being told, the compiler
-// keeps what follows from them there, descriptors too.)
-__device__ __forceinline__ bool amx_place(const AmxArgs &a, int &tile, int &split, int &b, int &h) {
-    const int n_groups = a.kv.batch * a.kv.Hkv, i = blockIdx.x >> 3;
-    const int set = __builtin_amdgcn_readfirstlane(i / a.n_tiles), unit = (blockIdx.x & 7) + 8 * set;
-    tile = i - set * a.n_tiles;
-    split = __builtin_amdgcn_readfirstlane(unit / n_groups);
-    const int group = unit - split * n_groups;
-    b = __builtin_amdgcn_readfirstlane(group / a.kv.Hkv);
-    h = group - b * a.kv.Hkv;
-    return split < a.n_splits;
+__device__ __forceinline__ uint32_t amx_sum(uint32_t x) {                       // over the wave: rows of 16 lanes by rotation, then the four rows
+    x += __builtin_amdgcn_update_dpp(0, x, 0x121, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x122, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x124, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, false);
+    return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) + __builtin_amdgcn_readlane(x, 32) + __builtin_amdgcn_readlane(x, 48);
+}
+__device__ __forceinline__ uint32_t amx_running_sum(uint32_t x, int lane) {     // of this lane and those before it
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);             // (row_shr 1, 2, 4, 8: 0 comes in)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+    const uint32_t r0 = __builtin_amdgcn_readlane(x, 15), r1 = r0 + __builtin_amdgcn_readlane(x, 31), r2 = r1 + __builtin_amdgcn_readlane(x, 47);
+    return x + (lane < 16 ? 0 : lane < 32 ? r0 : lane < 48 ? r1 : r2);
+}
+
+// What a workgroup does: a tile of queries of K/V head h of sequence b, over chunks first .. end of its keys (the cache's, the prefix', the pass rows'; KEYS a chunk, TURN
+// chunks at a time), which are one share of all.
+//
+// The shares are cut from the lengths that are there, not from the hint: of all sequences together as many as the host has workgroups for, none longer than it has
+// to be.  With c_b turns in sequence b, p of them a share, there are sum ceil(c_b / p) <= T / p + batch (1 - 1 / p) shares, T = sum c_b: p is at
+// least T / shares, and T / (shares - batch + 1) is enough; between the two every wave looks for the smallest that fits, the sequences in its lanes.  A batch of more than
+// a wave's lanes is cut by the hint: it has workgroups enough.
+struct AmxPlace { int tile, share, b, h, first, end, length; };
+// The arguments for a kernel's end, read again there: kept through the loops, scalar registers spilled.
+__device__ __forceinline__ AmxArgs amx_again() {
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    AmxArgs a;
+    __builtin_memcpy(&a, (const void *)p, sizeof a);
+    return a;
+}
+template <int KEYS, int TURN>
+__device__ __forceinline__ bool amx_place(const AmxArgs &a, AmxPlace &w) {
+    // The tiles that read the same keys go to one XCD, one behind the other: ids go round over the 8 XCDs.  (Quotients are worked out in vector registers: without
+    // being told, the compiler keeps what follows from them there, descriptors too.)
+    const int i = blockIdx.x >> 3, set = __builtin_amdgcn_readfirstlane(i / a.n_tiles), unit = (blockIdx.x & 7) + 8 * set;
+    w.tile = __builtin_amdgcn_readfirstlane(i - set * a.n_tiles);
+    w.share = __builtin_amdgcn_readfirstlane(unit / a.kv.Hkv);
+    w.h = __builtin_amdgcn_readfirstlane(unit - w.share * a.kv.Hkv);
+    if (w.share >= a.n_shares) return false;
+    const int batch = a.kv.batch, more = (a.P + KEYS - 1) / KEYS + (a.R - 1) / KEYS + 1, lane = threadIdx.x & 63;
+    auto turns = [&](int n) __attribute__((always_inline)) { return (uint32_t)((n + KEYS - 1) / KEYS + more + TURN - 1) / TURN; };
+    uint32_t per, mine, count, at;
+    if (a.n_shares == batch) {
+        w.b = w.share;
+        w.length = __builtin_amdgcn_readfirstlane(a.length(w.b));
+        w.first = 0;
+        w.end = INT_MAX;
+        return true;
+    }
+    if (batch > 64) {
+        mine = __builtin_amdgcn_readfirstlane(w.share / batch);
+        w.b = at = w.share - mine * batch;
+        w.length = __builtin_amdgcn_readfirstlane(a.length(w.b));
+        per = a.per_share;
+        count = __builtin_amdgcn_readfirstlane((turns(w.length) + per - 1) / per);
+        if (mine >= count) return false;
+    } else {
+        const int len = lane < batch ? a.length(lane) : 0;
+        const uint32_t c = lane < batch ? turns(len) : 0, all = amx_sum(c), shares = a.n_shares;
+        per = __builtin_amdgcn_readfirstlane((all + shares - 1) / shares);
+        uint32_t enough = __builtin_amdgcn_readfirstlane((all + shares - batch) / (shares - batch + 1));
+        while (per < enough) {
+            const uint32_t p = (per + enough) / 2;
+            if (amx_sum((c + p - 1) / p) <= shares) enough = p;
+            else per = p + 1;
+        }
+        const uint32_t n = (c + per - 1) / per, behind = amx_running_sum(n, lane);
+        const uint64_t later = __builtin_amdgcn_ballot_w64(behind > (uint32_t)w.share);
+        if (later == 0) return false;
+        w.b = __builtin_ctzll(later);
+        count = __builtin_amdgcn_readlane(n, w.b);
+        at = __builtin_amdgcn_readlane(behind, w.b) - count;
+        mine = w.share - at;
+        w.length = __builtin_amdgcn_readlane(len, w.b);
+    }
+    w.b = __builtin_amdgcn_readfirstlane(w.b);
+    w.length = __builtin_amdgcn_readfirstlane(w.length);
+    w.first = __builtin_amdgcn_readfirstlane(mine * per * TURN);
+    w.end = __builtin_amdgcn_readfirstlane(w.first + per * TURN);
+    if (mine == 0 && w.h == 0 && w.tile == 0 && threadIdx.x == 0) a.share_of[w.b] = make_int2(at, count);
+    return true;
 }
 
 // Sixteen neighbouring keys' codes and scale bytes, from one page or the contiguous cache: lane (g, c) = (l / 16, l % 16) takes a quarter of key c,
@@ -124,11 +203,9 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int Hkv = a.kv.Hkv;
-    int tile, split, b, h;
-    if (!amx_place(a, tile, split, b, h)) return;
-    const int Lc = __builtin_amdgcn_readfirstlane(min(max(a.ctx_len[b], 0), min(a.ctx_hint, a.kv.smax)));
-    const int nq = a.R * a.qpk;
+    AmxPlace at;
+    if (!amx_place<AMX_CHUNK, W>(a, at)) return;
+    const int tile = at.tile, b = at.b, h = at.h, Lc = at.length, nq = a.R * a.qpk;
 
     // queries: lane (g, c) holds, of query c of every tile, values VPL g + 8 s .. +8 of k-step s
     // (a query's row is worked out again where it is needed: kept through the loop it costs the registers that two tiles do not have)
@@ -136,14 +213,14 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
 #pragma unroll
     for (int u = 0; u < U; u++) {
         const int qc = min((tile * U + u) * 16 + c, nq - 1), row = qc / a.qpk, head = h * a.qpk + (qc - row * a.qpk);
-        const uint16_t *src = a.q + (((int64_t)b * a.R + row) * (a.qpk * Hkv) + head) * HD + VPL * g;
+        const uint16_t *src = a.q + a.query(b, row, head) * HD + VPL * g;
 #pragma unroll
         for (int s = 0; s < KS; s++) qf[u][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(src + 8 * s));
     }
     const int last_row = min((tile + 1) * U * 16 - 1, nq - 1) / a.qpk;          // of the workgroup: pass rows behind it are nobody's ancestors
 
     const int n_p = (a.P + AMX_CHUNK - 1) / AMX_CHUNK, n_c = (Lc + AMX_CHUNK - 1) / AMX_CHUNK, n_r = last_row / AMX_CHUNK + 1;
-    const int first = split * a.per_split + wave, end = min(n_c + n_p + n_r, (split + 1) * a.per_split);
+    const int first = at.first + wave, end = min(n_c + n_p + n_r, at.end);
 
     f32x4 o[U][NT];
     float m_run[U], base[U], l_run[U];
@@ -384,12 +461,13 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
             region[((u * W + wave) * NT + n) * 64 + lane] = make_float4(o[u][n][0] * f, o[u][n][1] * f, o[u][n][2] * f, o[u][n][3] * f);
     }
     __syncthreads();
+    const AmxArgs z = amx_again();
 #pragma unroll
     for (int u = 0; u < U; u++) {
-        const int qi = (tile * U + u) * 16 + c, row = qi / a.qpk;
+        const int qi = (tile * U + u) * 16 + c, row = qi / z.qpk;
         if (qi >= nq) continue;
-        const bool absent = a.token && !a.t.is_mask[row] && a.token[(int64_t)b * a.R + row] < 0;
-        const int64_t qrow = ((int64_t)b * a.R + row) * (a.qpk * Hkv) + h * a.qpk + (qi - row * a.qpk);
+        const bool absent = z.token && !z.t.is_mask[row] && z.token[(int64_t)b * z.R + row] < 0;
+        const int head = h * z.qpk + (qi - row * z.qpk);
 #pragma unroll
         for (int n = wave; n < NT; n += W) {
             float4 x = region[(u * W * NT + n) * 64 + lane];
@@ -398,16 +476,16 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
                 const float4 y = region[((u * W + w) * NT + n) * 64 + lane];
                 x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
             }
-            if (a.n_splits > 1) {
-                *reinterpret_cast<float4 *>(a.part_o + (qrow * a.n_splits + split) * HD + 16 * n + 4 * g) = x;
-                if (n == 0 && g == 0)
-                    *reinterpret_cast<float2 *>(a.part_ml + (qrow * a.n_splits + split) * 2) = absent ? make_float2(-INFINITY, 0.f) : make_float2(m_tot[u], l_tot[u]);
+            if (z.n_shares > z.kv.batch) {
+                const int64_t to = z.part(at.share, row, head);
+                *reinterpret_cast<float4 *>(z.part_o + to * HD + 16 * n + 4 * g) = x;
+                if (n == 0 && g == 0) *reinterpret_cast<float2 *>(z.part_ml + to * 2) = absent ? make_float2(-INFINITY, 0.f) : make_float2(m_tot[u], l_tot[u]);
                 continue;
             }
             // (a NaN sum stays one; a sum of nothing, or an absent row, gives zeros)
             const float inv = absent || l_tot[u] == 0.f ? 0.f : 1.0f / l_tot[u];
             const uint2 w2 = absent ? make_uint2(0, 0) : make_uint2(amx_pk_bf16(x.x * inv, x.y * inv), amx_pk_bf16(x.z * inv, x.w * inv));
-            *reinterpret_cast<uint2 *>(a.out + qrow * HD + 16 * n + 4 * g) = w2;
+            *reinterpret_cast<uint2 *>(z.out + z.query(b, row, head) * HD + 16 * n + 4 * g) = w2;
         }
     }
 }
@@ -423,27 +501,31 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
     using Keys = MxKeys<HD, BITS>;
     constexpr int TILE = Core::TILE, VPL = HD / 4, PARTS = Keys::PARTS;         // values a lane holds of a row: PARTS columns of 8
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];      // K tiles [2], V tiles [2]
-    const int lane = threadIdx.x & 63, hf = lane >> 5, c = lane & 31, g16 = lane >> 4, c16 = lane & 15;
+    const int lane = threadIdx.x & 63, hf = lane >> 5, g16 = lane >> 4, c16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int Hkv = a.kv.Hkv;
-    int tile, split, b, h;
-    if (!amx_place(a, tile, split, b, h)) return;
-    const int Lc = __builtin_amdgcn_readfirstlane(min(max(a.ctx_len[b], 0), min(a.ctx_hint, a.kv.smax)));
-    const int nq = a.R * a.qpk, qi = tile * AMW_ROWS + wave * 32 + c, qc = min(qi, nq - 1);
+    AmxPlace at;
+    if (!amx_place<CORE_KEYS, 1>(a, at)) return;
+    const int tile = at.tile, b = at.b, h = at.h, Lc = at.length;
+    const int nq = a.R * a.qpk;
     const bool idle = tile * AMW_ROWS + wave * 32 >= nq;                        // (it decodes all the same)
-    // (a query's row is worked out again where it is needed: kept through the loop it costs registers that are not there)
-    auto row_of = [&](int q) __attribute__((always_inline)) { asm volatile("" : "+v"(q)); return q / a.qpk; };
-    auto query_of = [&](int q, int row) __attribute__((always_inline)) { return ((int64_t)b * a.R + row) * (a.qpk * Hkv) + h * a.qpk + (q - row * a.qpk); };
+    // (what a lane is for, a query's row and its offsets, is worked out where it is used: kept through the loop, 8 bits of 128 spilled)
+    auto lane_now = [&]() __attribute__((always_inline)) {
+        int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    auto query_now = [&]() __attribute__((always_inline)) { return min(tile * AMW_ROWS + wave * 32 + (lane_now() & 31), nq - 1); };
 
     Core core;
     core.init(lane);
+    const int q_first = query_now(), q_at = q_first / a.qpk;
+    const uint16_t *q_row = a.q + a.query(b, q_at, h * a.qpk + (q_first - q_at * a.qpk)) * HD;
 #pragma unroll
-    for (int s = 0; s < Core::KS; s++)
-        core.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(a.q + query_of(qc, row_of(qc)) * HD + 16 * s + 8 * hf));
+    for (int s = 0; s < Core::KS; s++) core.q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(q_row + 16 * s + 8 * hf));
 
     const int last_row = min((tile + 1) * AMW_ROWS - 1, nq - 1) / a.qpk;        // of the workgroup: pass rows behind it are nobody's ancestors
     const int n_c = (Lc + CORE_KEYS - 1) / CORE_KEYS, n_p = (a.P + CORE_KEYS - 1) / CORE_KEYS, n_all = n_c + n_p + last_row / CORE_KEYS + 1;
-    const int begin = split * a.per_split, end = min(n_all, begin + a.per_split), c_end = min(end, n_c);
+    const int begin = at.first, end = min(n_all, at.end), c_end = min(end, n_c);
 
     const uint32_t lds = (uint32_t)(size_t)((__attribute__((address_space(3))) unsigned char *)smem);
     auto k_tile = [&](int t) __attribute__((always_inline)) { return lds + (t & 1) * TILE; };
@@ -462,12 +544,6 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
 #pragma unroll
         for (int s = 0; s < PARTS; s++) *(__attribute__((address_space(3))) u32x4_t *)(uintptr_t)(at ^ (16 * s)) = __builtin_bit_cast(u32x4_t, x[s]);
     };
-    // (the lane's offsets are worked out where they are used: kept through the loop, 8 bits of 128 spilled)
-    auto lane_now = [&]() __attribute__((always_inline)) {
-        int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-        asm volatile("" : "+v"(l));
-        return l;
-    };
     auto first_key = [&](int t) __attribute__((always_inline)) { return t * CORE_KEYS + 16 * wave; };
     auto load_k = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.k, a.kv.k_scale, h, first_key(t), Lc, page, Keys::code_offset(lane_now()), Keys::scale_offset(lane_now())); };
     auto load_v = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.v, a.kv.v_scale, h, first_key(t), Lc, page, Keys::code_offset(lane_now()), Keys::scale_offset(lane_now())); };
@@ -481,7 +557,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
     auto decode_v = [&](const Keys &x, int t) __attribute__((always_inline)) { decode(x, v_tile(t), true); };
     // scores of keys that `sees` has no bit for: none
     auto mask = [&](f32x16 (&s)[2], uint64_t sees) __attribute__((always_inline)) {
-        sees >>= 4 * hf;
+        sees >>= 4 * (lane_now() >> 5);
 #pragma unroll
         for (int e = 0; e < 32; e++) {
             const uint32_t w = (uint32_t)(sees >> (e & 16 ? 32 : 0));
@@ -536,7 +612,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
         t++;
     }
     // ---- the prefix and the pass' rows: bf16, not seen by every query
-    const int t_odd = t, row = row_of(qc);
+    const int t_odd = t;
     auto rows_of = [&](int t, const uint16_t *&k, const uint16_t *&v, int64_t &ldk, int64_t &ldv, int &n, uint64_t &sees) __attribute__((always_inline)) {
         const bool in_prefix = t < n_c + n_p;
         const int key0 = CORE_KEYS * (in_prefix ? t - n_c : t - n_c - n_p);
@@ -547,6 +623,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
         k += key0 * ldk;
         v += key0 * ldv;
         n = (in_prefix ? a.P : a.R) - key0;
+        const int row = query_now() / a.qpk;
         sees = (in_prefix ? (a.t.is_mask[row] ? ~0ull : 0) : a.t.anc[(int64_t)row * a.t.words + (key0 >> 6)]) & up_to(n);
     };
     for (; t < end; t++) {
@@ -555,12 +632,12 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
         int n;
         uint64_t sees;
         rows_of(t, k, v, ldk, ldv, n, sees);
-        const int r = min(my, n - 1);
+        const int l = lane_now(), r = min(16 * wave + (l & 15), n - 1), first = VPL * (l >> 4);
         bf16x8 x[PARTS], y[PARTS];
 #pragma unroll
         for (int i = 0; i < PARTS; i++) {
-            x[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(k + r * ldk + VPL * g16 + 8 * i));
-            y[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(v + r * ldv + VPL * g16 + 8 * i));
+            x[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(k + r * ldk + first + 8 * i));
+            y[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(v + r * ldv + first + 8 * i));
         }
         meet();
         put(k_tile(t), false, x);
@@ -582,25 +659,28 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
             core.add_nonfinite(v, ldv, n - 1, sees);
         }
 
+    const int end_lane = lane_now(), qi = tile * AMW_ROWS + wave * 32 + (end_lane & 31), half = end_lane >> 5;
     if (qi >= nq) return;
-    const int64_t qrow = query_of(qi, row);
+    const AmxArgs z = amx_again();
+    const int row = qi / z.qpk, head = h * z.qpk + (qi - row * z.qpk);
     const float l = core_sum_halves(core.l_run);
-    const bool absent = a.token && !a.t.is_mask[row] && a.token[(int64_t)b * a.R + row] < 0;
-    if (a.n_splits > 1) {                                                       // unnormalised: for attn_mx_merge_kernel
+    const bool absent = z.token && !z.t.is_mask[row] && z.token[(int64_t)b * z.R + row] < 0;
+    if (z.n_shares > z.kv.batch) {                                              // unnormalised: for attn_mx_merge_kernel
         // The sum's own power of two goes to the exponent: shares are weighed by what they hold, whatever reference they used (0 for what is no number).
         const int e = __builtin_amdgcn_frexp_expf(l);
-        float *dst = a.part_o + (qrow * a.n_splits + split) * HD + 4 * hf;
+        const int64_t to = z.part(at.share, row, head);
+        float *dst = z.part_o + to * HD + 4 * half;
 #pragma unroll
         for (int n = 0; n < Core::NT; n++)
 #pragma unroll
             for (int i = 0; i < 4; i++)
                 *reinterpret_cast<float4 *>(dst + 32 * n + 8 * i) =
                     make_float4(ldexpf(core.o[n][4 * i], -e), ldexpf(core.o[n][4 * i + 1], -e), ldexpf(core.o[n][4 * i + 2], -e), ldexpf(core.o[n][4 * i + 3], -e));
-        if (hf == 0) *reinterpret_cast<float2 *>(a.part_ml + (qrow * a.n_splits + split) * 2) = absent || l == 0.f ? make_float2(-INFINITY, 0.f) : make_float2(core.base + e, ldexpf(l, -e));
+        if (half == 0) *reinterpret_cast<float2 *>(z.part_ml + to * 2) = absent || l == 0.f ? make_float2(-INFINITY, 0.f) : make_float2(core.base + e, ldexpf(l, -e));
         return;
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    uint16_t *dst = a.out + qrow * HD + 4 * hf;
+    uint16_t *dst = z.out + z.query(b, row, head) * HD + 4 * half;
 #pragma unroll
     for (int n = 0; n < Core::NT; n++)
 #pragma unroll
@@ -614,14 +694,18 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
 // in a workgroup of 256 or more threads as many queries as there is room for).  A share without keys for the query has m = -inf and is left out
 // (nothing of it need have been written).  Bound by what the shares left in memory.
 template <int HD, int SIDE, int THREADS>
-__global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, int64_t n_queries, int n_splits,
-                                                                uint16_t *__restrict__ out) {
+__global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, const int2 *__restrict__ share_of, int64_t n_queries,
+                                                                int of_sequence, int stride, int n_shares, uint16_t *__restrict__ out) {
     constexpr int LANES = HD / 4, QUERIES = THREADS / (LANES * SIDE);
     const int i = threadIdx.x % LANES, side = threadIdx.x / LANES % SIDE, mine = threadIdx.x / (LANES * SIDE);
     const int64_t qrow = (int64_t)blockIdx.x * QUERIES + mine;
     const bool ok = qrow < n_queries;
-    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + (ok ? qrow : 0) * n_splits;
-    const float4 *po = reinterpret_cast<const float4 *>(part_o + (ok ? qrow : 0) * n_splits * HD) + i;
+    const int b = (uint32_t)(ok ? qrow : 0) / (uint32_t)of_sequence;            // (there are fewer than 2^27 queries)
+    const int2 shares = share_of[b];
+    const int n_splits = n_shares ? n_shares : shares.y;                        // (one sequence: its parts are on their way before it is known how many there are)
+    const int64_t part = (int64_t)(n_shares ? 0 : shares.x) * of_sequence + ((ok ? qrow : 0) - (int64_t)b * of_sequence), step = (int64_t)stride * of_sequence;
+    const float2 *ml = reinterpret_cast<const float2 *>(part_ml) + part;
+    const float4 *po = reinterpret_cast<const float4 *>(part_o + part * HD) + i;
     float m = -INFINITY, l = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s0 = side; s0 < n_splits; s0 += 4 * SIDE) {                        // four shares of a thread at a time, against their own maximum
@@ -630,9 +714,9 @@ __global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__r
 #pragma unroll
         for (int k = 0; k < 4; k++) {
             const int s = min(s0 + k * SIDE, n_splits - 1);
-            e[k] = ml[s];
-            o[k] = po[(int64_t)s * LANES];
-            if (s0 + k * SIDE >= n_splits) e[k].x = -INFINITY;
+            e[k] = ml[s * step];
+            o[k] = po[s * step * LANES];
+            if (s0 + k * SIDE >= shares.y) e[k].x = -INFINITY;
         }
         const float m_new = fmaxf(fmaxf(fmaxf(e[0].x, e[1].x), fmaxf(e[2].x, e[3].x)), m);
         if (m_new == -INFINITY) continue;
@@ -676,33 +760,36 @@ __global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__r
         m == -INFINITY ? make_uint2(0, 0) : make_uint2(amx_pk_bf16(x.x * inv, x.y * inv), amx_pk_bf16(x.z * inv, x.w * inv));
 }
 template <int HD>
-static void launch_merge(const AmxArgs &a, int64_t queries, int n_splits, hipStream_t s) {
+static void launch_merge(const AmxArgs &a, int64_t queries, hipStream_t s) {
+    const int of_sequence = a.R * a.qpk * a.kv.Hkv, stride = a.kv.batch > 64 ? a.kv.batch : 1, n = (a.n_shares + a.kv.batch - 1) / a.kv.batch, one = a.kv.batch == 1 ? a.n_shares : 0;
     // few shares: a thread takes them all; many: 8 or 32 rows of threads share them
-    if (n_splits <= 8) hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 1, 256>), dim3((unsigned)((queries * HD / 4 + 255) / 256)), dim3(256), 0, s, a.part_o, a.part_ml, queries, n_splits, a.out);
-    else if (n_splits <= 32) hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 8, 256>), dim3((unsigned)((queries * HD / 4 * 8 + 255) / 256)), dim3(256), 0, s, a.part_o, a.part_ml, queries, n_splits, a.out);
-    else hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 32, HD * 8>), dim3((unsigned)queries), dim3(HD * 8), 0, s, a.part_o, a.part_ml, queries, n_splits, a.out);
+    if (n <= 8) hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 1, 256>), dim3((unsigned)((queries * HD / 4 + 255) / 256)), dim3(256), 0, s, a.part_o, a.part_ml, a.share_of, queries, of_sequence, stride, one, a.out);
+    else if (n <= 32) hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 8, 256>), dim3((unsigned)((queries * HD / 4 * 8 + 255) / 256)), dim3(256), 0, s, a.part_o, a.part_ml, a.share_of, queries, of_sequence, stride, one, a.out);
+    else hipLaunchKernelGGL((attn_mx_merge_kernel<HD, 32, HD * 8>), dim3((unsigned)queries), dim3(HD * 8), 0, s, a.part_o, a.part_ml, a.share_of, queries, of_sequence, stride, one, a.out);
 }
 
-struct AmxPlan { bool wide; int tiles_u, waves, n_tiles, splits, per_split; int64_t workgroups; size_t part_o, part_ml; };
+struct AmxPlan { bool wide; int tiles_u, waves, n_tiles, shares, per_share; int64_t workgroups; size_t part_o, part_ml, total; };
 
-// How a launch is cut, from nothing but its sizes: 16 queries a workgroup of 8 waves or of 4, 32 queries, or 128 that share decoded keys (wide); and the keys into
-// shares, which go by the hint, so that shorter sequences of a batch have fewer of them.  The estimate behind the choice, in us at head_dim 128:
+// How a launch is cut, from nothing but its sizes: 16 queries a workgroup of 8 waves or of 4, 32 queries, or 128 that share decoded keys (wide); and how many shares the
+// keys of all sequences are split into (as many as sequences: not at all).  The estimate behind the choice, in us at head_dim 128:
 //   a round of workgroups: their start and end, and their turns (256 keys, 128, 128, 64) at the pace of one workgroup a CU or of as many as a CU holds, but no faster
 //   than a CU takes codes in, 35 KB a us; the bytes that all of them read at 6 TB/s, 5 where tiles of queries read the same ones again (of these two the longer, and a
 //   quarter of the other); and, where the keys are split, a second kernel and what the shares write and read, at 4.5 TB/s.
+// Split launches fill the card once.  A batch's lengths are taken to be half to three quarters of the hint on average; not split, its longest decides.
 // Measured (16 queries in 4 waves / 32 / wide): a turn with one workgroup a CU 0.9 / 1.25 / 1.56 us, with two 1.44 / 2.1 / 2.43; the start and end 5.6 / 5.6 / 7; a turn of
-// 8 waves 1.0.  A batch's lengths are taken to be half to three quarters of the hint on average.  Each kind with its best shares, 16 queries in 8 waves / in 4 / 32 / wide:
-//   68 rows, 32 heads of their own keys, 1024 keys of 4 bits 11.8 / 14.2 / 16.1 / 19.1 us; 4096 keys of 8 bits 41.8 / 40.7 / 28.4 / 24.1; four sequences of 400 to 1100
-//   keys 31.2 / 21.6 / 30.3 / 28.5; 4 sequences of 1024 to 4096 keys, 64/8 heads 145 / 127 / 81 / 57; 20 rows there 38.4 / 34.5 / 30.5 / 40.4; single tokens: 32 sequences
-//   of up to 8192 keys 42.8 / 35.7 / 47 / 82; one of 131072 keys of 4 bits 31.2 / 36.6 / 41.2 / 59; one of 1000, 32 heads 10.2 / 9.3 / 9.7 / 11.3 (the last three with
+// 8 waves 1.0.  Each kind with its best shares, 16 queries in 8 waves / in 4 / 32 / wide:
+//   68 rows, 32 heads of their own keys, 1024 keys of 4 bits 12.0 / 14.4 / 16.1 / 20.1 us; 4096 keys of 8 bits 43 / 41 / 30 / 25; four sequences of 400 to 1100
+//   keys 31.9 / 21.7 / 30.8 / 32.1; 4 sequences of 1024 to 4096 keys, 64/8 heads 146 / 127 / 83 / 56; 20 rows there 39 / 32 / 31 / 34; single tokens: 32 sequences
+//   of up to 8192 keys 42 / 33.4 / 44 / 67; one of 131072 keys of 4 bits 32 / 37 / 42 / 62; one of 1000, 32 heads 10.2 / 10.2 / 10.6 / 12 (the last three with
 //   a second kernel, whose launch costs the host as much again: hence 3.5 us for it, more than its own time).
+// With shares cut from the hint instead, 8 sequences of 100 to 4000 keys of 8 bits, 32 heads, took 43 us (now 29), 3 of 0 to 39168, 6/2 heads 28 (17), 30 of 0 to
+// 26000 45 (37), the 32 above 36.
 static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int bits, int ctx_hint, int n_prompt) {
     static const struct { int queries, unit, waves, slots; double start, one, many; } kinds[4] = {
         {16, AMX_CHUNK, 8, 256, 5.6, 1.0, 1.0}, {16, AMX_CHUNK, 4, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, 4, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 4, 512, 7.0, 1.56, 2.43}};
-    static const int shares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128, 192, 256};
-    const int64_t nq = (int64_t)rows * (Hq / Hkv), queries = (int64_t)batch * rows * Hq;
-    const double fill = batch > 1 ? 0.75 : 1.0, size = hd / 128.0;
-    const double key_bytes = 2 * (hd * bits / 8 + hd / 32), cache = (double)batch * Hkv * ctx_hint * (batch > 1 ? 0.5 : 1.0) * key_bytes;
+    static const int per_sequence[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128, 192, 256};
+    const int64_t nq = (int64_t)rows * (Hq / Hkv);
+    const double size = hd / 128.0, key_bytes = 2 * (hd * bits / 8 + hd / 32), cache = (double)batch * Hkv * ctx_hint * (batch > 1 ? 0.5 : 1.0) * key_bytes;
     AmxPlan p = {};
     double best = 1e300;
     for (int k = 0; k < (nq <= 16 ? 2 : nq <= 32 ? 3 : 4); k++) {
@@ -710,31 +797,46 @@ static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int bits, 
         const int unroll = k == 3 ? 1 : kind.waves;                             // chunks of a turn
         const int n_tiles = (int)((nq + kind.queries - 1) / kind.queries);
         auto units = [&](int64_t n) { return (n + kind.unit - 1) / kind.unit; };
-        const int64_t chunks = units(n_prompt) + units(ctx_hint) + units(rows), wgs = (int64_t)batch * Hkv * n_tiles;
-        for (int want : shares) {
-            if (want > 1 && want * unroll > chunks) break;
-            const int64_t turns = (chunks + (int64_t)want * unroll - 1) / ((int64_t)want * unroll), per = turns * unroll, splits = (chunks + per - 1) / per;
-            const double busy = (double)(wgs * splits) * (k ? fill : 1.0);         // (alone on a CU, a short workgroup leaves it to the next one late)
-            const double rounds = k && batch > 1 ? std::max(busy / kind.slots, 1.0) : (double)((wgs * splits + kind.slots - 1) / kind.slots);
+        auto turns_of = [&](int64_t n) { return (units(n_prompt) + units(n) + units(rows) + unroll - 1) / unroll; };
+        const int64_t longest = turns_of(ctx_hint), usual = turns_of(batch > 1 ? (int64_t)(0.6 * ctx_hint) : ctx_hint), share_wgs = (int64_t)Hkv * n_tiles;
+        auto consider = [&](int64_t shares, int64_t per) {
+            const bool split = shares > batch;
+            const int64_t wgs = shares * share_wgs;
+            const double turns = !split ? (double)longest : batch > 64 ? (double)per : (double)(usual * batch + shares - 1) / shares + (batch > 1 ? 0.5 : 0.0);
+            // (not split, a batch's short sequences leave room for others; alone on a CU, a workgroup leaves it to the next one late)
+            const double busy = (double)wgs * (k && batch > 1 && (!split || batch > 64) ? 0.75 : 1.0);
+            const double rounds = k && batch > 1 ? std::max(busy / kind.slots, 1.0) : (double)((wgs + kind.slots - 1) / kind.slots);
             const double on_a_cu = std::min(busy < 256 ? 1.0 : busy / 256, kind.slots / 256.0);
             const double turn = std::max(size * (busy <= 256 ? kind.one : kind.many), on_a_cu * unroll * kind.unit * key_bytes / 35e3);
-            const double pace = rounds * (double)turns * turn, load = cache * n_tiles / (n_tiles > 1 ? 5e6 : 6e6);
+            const double pace = rounds * turns * turn, load = cache * n_tiles / (n_tiles > 1 ? 5e6 : 6e6);
             double us = rounds * kind.start + std::max(pace, load) + 0.25 * std::min(pace, load);
-            if (splits > 1) us += 3.5 + 0.03 * (double)splits + (double)(queries * splits) * fill * hd * 8 / 4.5e6;
+            if (split) us += 3.5 + 0.03 * (double)shares / batch + (double)shares * rows * Hq * hd * 8 / 4.5e6;
             if (us < best) {
                 best = us;
                 p.wide = k == 3;
                 p.tiles_u = k < 2 ? 1 : 2;
                 p.waves = kind.waves;
                 p.n_tiles = n_tiles;
-                p.splits = (int)splits;
-                p.per_split = (int)per;
-                p.workgroups = wgs * splits;
+                p.shares = (int)shares;
+                p.per_share = (int)per;
+                p.workgroups = wgs;
             }
+        };
+        for (int want : per_sequence) {
+            const int64_t per = (longest + want - 1) / want, shares = (longest + per - 1) / per * batch;
+            if (want > 1 && (want > longest || shares * share_wgs > kind.slots * (batch > 64 ? 2 : 1))) break;
+            consider(shares, per);
         }
+        if (batch <= 64)                                                        // as many as a CU, or two of them, or three hold
+            for (int slots = 256; slots <= kind.slots; slots += 256)
+                if (slots / share_wgs > batch && slots / share_wgs <= batch * longest) consider(slots / share_wgs, 0);
     }
-    p.part_o = p.splits > 1 ? ((size_t)queries * p.splits * hd * 4 + 255) / 256 * 256 : 0;
-    p.part_ml = p.splits > 1 ? ((size_t)queries * p.splits * 8 + 255) / 256 * 256 : 0;
+    if (p.shares > batch) {
+        auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+        p.part_o = up((size_t)p.shares * rows * Hq * hd * 4);
+        p.part_ml = up((size_t)p.shares * rows * Hq * 8);
+        p.total = p.part_o + p.part_ml + up((size_t)batch * 8);
+    }
     return p;
 }
 
@@ -751,7 +853,7 @@ extern "C" size_t bita_tree_attention_mx_workspace_bytes(int32_t batch, int32_t 
                                                          int32_t ctx_hint, int32_t n_prompt) {
     if (amx_sizes("bita_tree_attention_mx_workspace_bytes", batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt)) return 0;
     const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt);
-    return p.part_o + p.part_ml;
+    return p.total;
 }
 
 extern "C" int bita_tree_attention_mx_plan_info(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t bits, int32_t ctx_hint,
@@ -759,22 +861,22 @@ extern "C" int bita_tree_attention_mx_plan_info(int32_t batch, int32_t rows, int
     if (!out4) return bita_set_error(BITA_ERR_INVALID_ARG, "bita_tree_attention_mx_plan_info: null argument");
     if (int rc = amx_sizes("bita_tree_attention_mx_plan_info", batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt)) return rc;
     const AmxPlan p = amx_plan(batch, rows, n_heads, n_kv_heads, head_dim, bits, ctx_hint, n_prompt);
-    out4[0] = p.splits; out4[1] = p.wide ? AMW_ROWS : 16 * p.tiles_u; out4[2] = p.waves;
+    out4[0] = (p.shares + batch - 1) / batch; out4[1] = p.wide ? AMW_ROWS : 16 * p.tiles_u; out4[2] = p.waves;
     out4[3] = p.workgroups < INT32_MAX ? (int32_t)p.workgroups : INT32_MAX;
     return BITA_OK;
 }
 
 template <int HD, int BITS>
-static void launch_amw(const AmxArgs &a, int64_t n_groups, hipStream_t s) {
-    const dim3 grid((unsigned)((n_groups * a.n_splits + 7) / 8 * 8 * a.n_tiles));
+static void launch_amw(const AmxArgs &a, int64_t n_units, hipStream_t s) {
+    const dim3 grid((unsigned)((n_units + 7) / 8 * 8 * a.n_tiles));
     hipLaunchKernelGGL((attn_mx_wide_kernel<HD, BITS>), grid, dim3(AMX_WAVES * 64), (4 * AttnCore<HD>::TILE), s, a);
 }
 template <int HD, int BITS, int U, int W>
-static void launch_amx(const AmxArgs &a, int64_t n_groups, hipStream_t s) {
+static void launch_amx(const AmxArgs &a, int64_t n_units, hipStream_t s) {
     constexpr int SMEM = AmxCfg<HD, U, W>::SMEM;
     static_assert(W / AMX_WAVES * SMEM <= 160 * 1024 && SMEM <= 80 * 1024, "two workgroups a CU");
     if (SMEM > 64 * 1024) (void)hipFuncSetAttribute((const void *)attn_mx_kernel<HD, BITS, U, W>, hipFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    const dim3 grid((unsigned)((n_groups * a.n_splits + 7) / 8 * 8 * a.n_tiles));
+    const dim3 grid((unsigned)((n_units + 7) / 8 * 8 * a.n_tiles));
     hipLaunchKernelGGL((attn_mx_kernel<HD, BITS, U, W>), grid, dim3(W * 64), SMEM, s, a);
 }
 
@@ -794,28 +896,28 @@ extern "C" int bita_tree_attention_mx(const bita_tree_template *t, const void *d
     if (int rc = mx_rows_check(who, a.k_at, a.v_at, (uintptr_t)d_q | (uintptr_t)d_k_rows | (uintptr_t)d_v_rows | (uintptr_t)d_prompt_k | (uintptr_t)d_prompt_v |
                                                         (uintptr_t)d_out | (uintptr_t)d_ws)) return rc;
     const AmxPlan p = amx_plan(kv->batch, t->dev.rows, n_heads, kv->n_kv_heads, kv->head_dim, kv->bits, ctx_hint, n_prompt);
-    if (ws_bytes < p.part_o + p.part_ml || (p.splits > 1 && !d_ws))
-        return bita_set_error(BITA_ERR_CAPACITY, "%s: workspace %zu < %zu bytes", who, ws_bytes, p.part_o + p.part_ml);
+    if (ws_bytes < p.total || (p.total && !d_ws)) return bita_set_error(BITA_ERR_CAPACITY, "%s: workspace %zu < %zu bytes", who, ws_bytes, p.total);
     a.t = t->dev;
     a.q = (const uint16_t *)d_q; a.k_rows = (const uint16_t *)d_k_rows; a.v_rows = (const uint16_t *)d_v_rows;
     a.prompt_k = (const uint16_t *)d_prompt_k; a.prompt_v = (const uint16_t *)d_prompt_v;
     a.ctx_len = d_ctx_len; a.token = d_token;
     a.P = n_prompt; a.R = t->dev.rows; a.qpk = n_heads / kv->n_kv_heads; a.ctx_hint = ctx_hint;
-    a.n_tiles = p.n_tiles; a.n_splits = p.splits; a.per_split = p.per_split;
+    a.n_tiles = p.n_tiles; a.n_shares = p.shares; a.per_share = p.per_share;
     a.scale_log2 = 1.4426950408889634f / sqrtf((float)kv->head_dim);
     a.part_o = (float *)d_ws; a.part_ml = (float *)((unsigned char *)d_ws + p.part_o);
+    a.share_of = (int2 *)((unsigned char *)d_ws + p.part_o + p.part_ml);
     a.out = (uint16_t *)d_out;
     hipStream_t s = (hipStream_t)stream;
-    const int64_t groups = (int64_t)kv->batch * kv->n_kv_heads;
-#define AMX_LAUNCH(HD_, BITS_) do { if (p.wide) launch_amw<HD_, BITS_>(a, groups, s); else if (p.tiles_u == 2) launch_amx<HD_, BITS_, 2, 4>(a, groups, s); \
-    else if (p.waves == 8) launch_amx<HD_, BITS_, 1, 8>(a, groups, s); else launch_amx<HD_, BITS_, 1, 4>(a, groups, s); } while (0)
+    const int64_t units = (int64_t)p.shares * kv->n_kv_heads;
+#define AMX_LAUNCH(HD_, BITS_) do { if (p.wide) launch_amw<HD_, BITS_>(a, units, s); else if (p.tiles_u == 2) launch_amx<HD_, BITS_, 2, 4>(a, units, s); \
+    else if (p.waves == 8) launch_amx<HD_, BITS_, 1, 8>(a, units, s); else launch_amx<HD_, BITS_, 1, 4>(a, units, s); } while (0)
     if (kv->head_dim == 128) { if (kv->bits == 4) AMX_LAUNCH(128, 4); else AMX_LAUNCH(128, 8); }
     else { if (kv->bits == 4) AMX_LAUNCH(64, 4); else AMX_LAUNCH(64, 8); }
 #undef AMX_LAUNCH
-    if (p.splits > 1) {
+    if (p.shares > kv->batch) {
         const int64_t queries = (int64_t)kv->batch * t->dev.rows * n_heads;
-        if (kv->head_dim == 128) launch_merge<128>(a, queries, p.splits, s);
-        else launch_merge<64>(a, queries, p.splits, s);
+        if (kv->head_dim == 128) launch_merge<128>(a, queries, s);
+        else launch_merge<64>(a, queries, s);
     }
     BITA_HIP_CHECK(hipGetLastError());
     return BITA_OK;

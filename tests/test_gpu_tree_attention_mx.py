@@ -260,21 +260,37 @@ def test_same_result_every_time_eager_and_replayed(bits):
             assert torch.equal(o, w)
 
 
-@BITS
-@pytest.mark.parametrize("cut,n,R,masks,hq,hkv,hd,ctx,page,P", [
-    ((16, 4, False), 2, 20, 4, 2, 2, 64, [40, 33], 16, 5),
-    ((16, 8, False), 1, 35, 3, 4, 4, 128, [300], 64, 16),       # three tiles a head that read the same keys
-    ((16, 8, True), 1, 33, 0, 2, 1, 64, [6000], 0, 40),
-    ((32, 4, False), 8, 20, 2, 32, 16, 64, [40, 39, 31, 0, 1, 33, 32, 17], 32, 3),
-    ((32, 4, True), 17, 5, 2, 8, 2, 128, [1500, 0, 1, 700, 64, 32, 33, 31, 900, 1499, 10, 128, 127, 129, 300, 256, 255], 64, 40),
-    ((128, 4, False), 17, 68, 4, 64, 2, 64, [40, 39, 31, 0, 1, 33, 32, 17, 40, 5, 6, 7, 8, 9, 10, 11, 12], 16, 3),
-    ((128, 4, True), 1, 130, 5, 16, 1, 128, [6000], 256, 16),
-])
-def test_every_cut_of_a_launch(bits, cut, n, R, masks, hq, hkv, hd, ctx, page, P):
-    """The kinds of workgroups, with one share of the keys and with several, and a NaN among the pass' values, which reaches the rows that see it only."""
+RAGGED = [1500, 0, 1, 700, 64, 32, 33, 31, 900, 1499, 10, 128, 127, 129, 300, 256, 255]
+CUTS = [
+    (2, 20, 4, 2, 2, 64, [40, 33], 16, 5),
+    (1, 35, 3, 4, 4, 128, [300], 64, 16),                         # three tiles a head that read the same keys
+    (1, 1, 0, 2, 1, 64, [3000], 0, 40),
+    (3, 1, 0, 2, 1, 128, [1500, 0, 31], 16, 0),                   # all shares but a few are one sequence's
+    (17, 5, 2, 8, 2, 128, RAGGED, 64, 40),
+    (70, 1, 0, 2, 1, 64, [(37 * i) % 1501 for i in range(70)], 16, 3),   # more sequences than a wave has lanes
+    (8, 20, 2, 32, 16, 64, [40, 39, 31, 0, 1, 33, 32, 17], 32, 3),
+    (1, 20, 2, 16, 16, 128, [1500], 0, 0),
+    (1, 20, 0, 32, 32, 128, [3000], 0, 0),
+    (17, 68, 4, 64, 2, 64, [40, 39, 31, 0, 1, 33, 32, 17, 40, 5, 6, 7, 8, 9, 10, 11, 12], 16, 3),
+    (1, 130, 5, 16, 1, 128, [6000], 256, 16),
+    (3, 130, 5, 16, 1, 128, [2000, 0, 900], 256, 70),
+]
+
+
+def cut_of(bits, n, R, masks, hq, hkv, hd, ctx, page, P):
     import paper_2401_12522_amd as bita
     plan = bita.binding.tree_attention_mx_plan_info(n, R, hq, hkv, hd, bits, max(ctx), P)
-    assert (plan["queries"], plan["waves"], plan["splits"] > 1) == cut
+    return plan["queries"], plan["waves"], plan["splits"] > 1
+
+
+def test_the_cases_below_are_cut_in_every_way():
+    assert {cut_of(b, *c) for b in (4, 8) for c in CUTS} == {(q, w, s) for q, w in ((16, 4), (16, 8), (32, 4), (128, 4)) for s in (False, True)}
+
+
+@BITS
+@pytest.mark.parametrize("n,R,masks,hq,hkv,hd,ctx,page,P", CUTS)
+def test_every_cut_of_a_launch(bits, n, R, masks, hq, hkv, hd, ctx, page, P):
+    """The kinds of workgroups, with one share of the keys a sequence and with several, and a NaN among the pass' values, which reaches the rows that see it only."""
     call, (out, tol), (cache, q, kr, vr, _, _, tmpl, seen, _) = case(n, R, masks, hq, hkv, hd, bits, ctx, page, P, seed=7)
     near(call(), out, tol)
     at = R - masks - 1
@@ -283,3 +299,34 @@ def test_every_cut_of_a_launch(bits, cut, n, R, masks, hq, hkv, hd, ctx, page, P
     assert torch.isnan(got[:, seen[:, at]][..., 3]).all()
     got[..., 3] = torch.where(seen[:, at][None, :, None], out[..., 3], got[..., 3])
     near(got, out, tol)
+
+
+@BITS
+@pytest.mark.parametrize("n,hint", [(1, 20000), (5, 20000), (70, 3000)])
+def test_shares_are_cut_from_the_lengths_not_the_hint(bits, n, hint):
+    """A launch for long sequences (as a captured graph holds it) over short ones, a few of them long, in turn: one workspace, another cut each time."""
+    import paper_2401_12522_amd as bita
+    tmpl, seen, is_mask = template(3)
+    cache, ck, cv = filled(1, 64, n, 700, bits, 0, 5)
+    cache = bita.KVCacheMX(1, 64, n, hint, bits=bits)
+    k, v = rows((n, 1, 700, 64), 6, torch.bfloat16), rows((n, 1, 700, 64), 7, torch.bfloat16)
+    bita.kv_write_mx(cache, k.cuda(), v.cuda(), i32([0] * n))
+    ck, cv = ref.rounded(k, bits), ref.rounded(v, bits)
+    q, kr, vr = rows((n, 3, 2, 64), 1, torch.bfloat16), rows((n, 1, 3, 64), 2, torch.bfloat16), rows((n, 1, 3, 64), 3, torch.bfloat16)
+    ws = torch.empty(bita.lib().bita_tree_attention_mx_workspace_bytes(n, 3, 2, 1, 64, bits, hint, 0), dtype=torch.uint8, device="cuda")
+    assert ws.numel() > 0
+    ctx = i32([0] * n)
+    qc, kc, vc, out = q.cuda(), kr.cuda(), vr.cuda(), torch.empty((n, 3, 128), dtype=torch.bfloat16, device="cuda")
+    call = lambda: bita.tree_attention_mx(tmpl, qc, cache, kc, vc, ctx, hint, out=out, workspace=ws)     # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for lengths in ([0] * n, [1] * (n - 1) + [700], [700] * n, [700] + [33] * (n - 1)):
+        ctx.copy_(i32(lengths))
+        want, tol = expected(q, ck, cv, kr, vr, lengths, seen, is_mask)
+        for step in (g.replay, call):
+            out.fill_(9.0)
+            step()
+            near(out, want, tol)
