@@ -71,7 +71,7 @@ def _spilling_products(resources):
     """The products' kernels, and those of the small cache's and the prompts' attention, are written to fit their register budget in every instantiation: a spill inside their loops is
     silent and costs percents of a step (scratch traffic shares the vector-memory path and its wait counter with the weight
     stream), so it fails the build instead."""
-    kernels = ("gemm_skinny_kernel", "gemm_q8_skinny_kernel", "gemm_q8_tile_kernel", "attn_mx_kernel", "prompt_attn_kernel")
+    kernels = ("gemm_skinny_kernel", "gemm_q8_skinny_kernel", "gemm_q8_tile_kernel", "attn_mx_", "prompt_attn_kernel")
     return sorted(k for k, v in resources.items() if v.get("scratch", 0) > 0 and any(n in k for n in kernels))
 
 
