@@ -47,7 +47,7 @@ struct AmxArgs {
     int P, R, qpk, ctx_hint, n_tiles, n_shares, per_share;      // tiles of a workgroup's queries; shares of all sequences' keys together (as many: nothing is split); turns of a share where the batch is large
     float scale_log2;
     float *part_o, *part_ml;                                    // [share][R * heads][HD], [..][2]
-    int2 *share_of;                                             // [batch]: a sequence's first share and how many it has
+    int2 *share_of;                                             // [batch]: a sequence's first share and how many it has (one: the result is in out)
     uint16_t *out;
     __device__ __forceinline__ int length(int b) const { return min(max(ctx_len[b], 0), min(ctx_hint, kv.smax)); }
     // of a query (row, head) of sequence b: where it is in out and q, and where in a share's part
@@ -78,7 +78,7 @@ __device__ __forceinline__ uint32_t amx_running_sum(uint32_t x, int lane) {     
 // to be.  With c_b turns in sequence b, p of them a share, there are sum ceil(c_b / p) <= T / p + batch (1 - 1 / p) shares, T = sum c_b: p is at
 // least T / shares, and T / (shares - batch + 1) is enough; between the two every wave looks for the smallest that fits, the sequences in its lanes.  A batch of more than
 // a wave's lanes is cut by the hint: it has workgroups enough.
-struct AmxPlace { int tile, share, b, h, first, end, length; };
+struct AmxPlace { int tile, share, b, h, first, end, length; bool split; };  // split: the sequence has other shares
 // The arguments for a kernel's end, read again there: kept through the loops, scalar registers spilled.
 __device__ __forceinline__ AmxArgs amx_again() {
     auto p = __builtin_amdgcn_kernarg_segment_ptr();
@@ -104,6 +104,7 @@ __device__ __forceinline__ bool amx_place(const AmxArgs &a, AmxPlace &w) {
         w.length = __builtin_amdgcn_readfirstlane(a.length(w.b));
         w.first = 0;
         w.end = INT_MAX;
+        w.split = false;
         return true;
     }
     if (batch > 64) {
@@ -136,6 +137,7 @@ __device__ __forceinline__ bool amx_place(const AmxArgs &a, AmxPlace &w) {
     w.length = __builtin_amdgcn_readfirstlane(w.length);
     w.first = __builtin_amdgcn_readfirstlane(mine * per * TURN);
     w.end = __builtin_amdgcn_readfirstlane(w.first + per * TURN);
+    w.split = __builtin_amdgcn_readfirstlane(count) > 1;
     if (mine == 0 && w.h == 0 && w.tile == 0 && threadIdx.x == 0) a.share_of[w.b] = make_int2(at, count);
     return true;
 }
@@ -476,7 +478,7 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
                 const float4 y = region[((u * W + w) * NT + n) * 64 + lane];
                 x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
             }
-            if (z.n_shares > z.kv.batch) {
+            if (at.split) {
                 const int64_t to = z.part(at.share, row, head);
                 *reinterpret_cast<float4 *>(z.part_o + to * HD + 16 * n + 4 * g) = x;
                 if (n == 0 && g == 0) *reinterpret_cast<float2 *>(z.part_ml + to * 2) = absent ? make_float2(-INFINITY, 0.f) : make_float2(m_tot[u], l_tot[u]);
@@ -665,7 +667,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
     const int row = qi / z.qpk, head = h * z.qpk + (qi - row * z.qpk);
     const float l = core_sum_halves(core.l_run);
     const bool absent = z.token && !z.t.is_mask[row] && z.token[(int64_t)b * z.R + row] < 0;
-    if (z.n_shares > z.kv.batch) {                                              // unnormalised: for attn_mx_merge_kernel
+    if (at.split) {                                                             // unnormalised: for attn_mx_merge_kernel
         // The sum's own power of two goes to the exponent: shares are weighed by what they hold, whatever reference they used (0 for what is no number).
         const int e = __builtin_amdgcn_frexp_expf(l);
         const int64_t to = z.part(at.share, row, head);
@@ -754,7 +756,7 @@ __global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__r
         }
         m = top;
     }
-    if (!ok) return;
+    if (!ok || shares.y == 1) return;                                           // (one share: it wrote the result itself)
     const float inv = 1.0f / l;
     *reinterpret_cast<uint2 *>(out + qrow * HD + 4 * i) =
         m == -INFINITY ? make_uint2(0, 0) : make_uint2(amx_pk_bf16(x.x * inv, x.y * inv), amx_pk_bf16(x.z * inv, x.w * inv));
