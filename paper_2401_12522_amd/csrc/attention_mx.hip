@@ -494,7 +494,9 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
 
 // Many queries a K/V head (a tree under grouped heads): a workgroup's waves own 32 queries each and share the keys, in tiles of 64 that they decode
 // together into LDS, each wave 16 rows, a tile ahead of the products (attention_core.h).  Scores run a tile ahead of the values too, so
-// K is decoded two tiles ahead and V one, from codes that were asked for a tile earlier.  A wave finishes its own queries.
+// K is decoded two tiles ahead and V one, from codes that were asked for a tile earlier.  A wave finishes its own queries.  Bound by exponentials, conversions and
+// matrix instructions together: a turn of two workgroups on a CU is 2.43 us, 884 TFLOP/s over the card (with one 1.56); four trees of 68 rows over 1024 to 4096 keys of 8 bits, 64/8
+// heads, 52 us, and 6.5 for the shares' sum.
 #define AMW_ROWS (32 * AMX_WAVES)
 
 template <int HD, int BITS>
@@ -694,7 +696,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
 
 // o = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max m): HD / 4 threads a query's columns, SIDE such rows of threads side by side its shares (and
 // in a workgroup of 256 or more threads as many queries as there is room for).  A share without keys for the query has m = -inf and is left out
-// (nothing of it need have been written).  Bound by what the shares left in memory.
+// (nothing of it need have been written).  Bound by what the shares left in memory: 12 shares of 4352 queries 6.5 us, 27 MB; few of them: by a launch and two ways to memory, 4.1.
 template <int HD, int SIDE, int THREADS>
 __global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, const int2 *__restrict__ share_of, int64_t n_queries,
                                                                 int of_sequence, int stride, int n_shares, uint16_t *__restrict__ out) {

@@ -3,7 +3,8 @@
 //
 // A thread holds 8 neighbouring values of a head's first half and the 8 they rotate with of the second (16-byte accesses in bf16), so a head is 8
 // (4) threads whose sums of squares meet in three (two) steps inside a row of lanes, and nothing else crosses a lane.  What bounds it is
-// what it moves, each value read and written once; at a row or two, the launch and two round trips to memory (position, then table).
+// what it moves, each value read and written once: 8192 rows of 64 + 8 heads of 128 in bf16, 306 MB, 59.8 us, 5.1 TB/s, a copy's rate (with 8-byte accesses and 1, 2 or
+// 4 heads a thread 72.5, 70.4 and 76.3 us); at a row or two, the launch and two round trips to memory (position, then table): 2.8 us.
 #include "common.h"
 #include <cmath>
 #include <type_traits>
