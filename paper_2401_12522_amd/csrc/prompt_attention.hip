@@ -11,7 +11,7 @@
 //  * Key tiles before a wave's queries need no mask.  Workgroups start with the longest walks.
 // Bound by matrix instructions at the clock that the card holds under them, with the exponentials between them: 8192 tokens of 64/8 heads of 128 1019 us, 1080 TFLOP/s
 // of what the mask leaves, 0.90 of the library's rate for a product of 8192^3; a turn of two workgroups on a CU 1.96 us.  Ragged prompts by the packing of their walks: 2049, 1411, 977,
-// 350 tokens and less of 32 heads 90 us, 74 of them a packing without starts and ends.  128 queries a workgroup and not 256, so that two of them fill each other's waits.
+// 350 tokens and less of 32 heads 90 us, 74 of them a packing without starts and ends.
 #include <cmath>
 #include <type_traits>
 #include "attention_core.h"

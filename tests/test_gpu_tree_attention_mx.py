@@ -330,3 +330,21 @@ def test_shares_are_cut_from_the_lengths_not_the_hint(bits, n, hint):
             out.fill_(9.0)
             step()
             near(out, want, tol)
+
+
+@BITS
+@pytest.mark.parametrize("n,R,masks,hq,hkv,hd,ctx,page,P", CUTS)
+def test_a_block_that_is_no_number_in_every_cut(bits, n, R, masks, hq, hkv, hd, ctx, page, P):
+    """A cached V block with an infinity reads back as NaN: 32 columns of its sequence and K/V head, and nothing else."""
+    import paper_2401_12522_amd as bita
+    call, (out, tol), (cache, q, kr, vr, ck, cv, *_) = case(n, R, masks, hq, hkv, hd, bits, ctx, page, P, seed=9)
+    b = max(range(n), key=lambda i: ctx[i])
+    slot = ctx[b] // 2
+    k, v = ck[:, :, slot: slot + 1].to(torch.bfloat16), cv[:, :, slot: slot + 1].to(torch.bfloat16)      # (what is there already, exact in bf16)
+    v[b, 0, 0, 35] = float("inf")
+    bita.kv_write_mx(cache, k.cuda(), v.cuda(), i32([slot] * n), i32([int(i == b) for i in range(n)]))
+    got = call().cpu().double().view(out.shape)
+    group = hq // hkv
+    assert torch.isnan(got[b, :, :group, 32:64]).all()
+    got[b, :, :group, 32:64] = out[b, :, :group, 32:64]
+    near(got, out, tol)
