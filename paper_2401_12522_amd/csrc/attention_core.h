@@ -163,7 +163,8 @@ struct AttnCore {
     // second, pair by pair.
     __device__ __forceinline__ void scores_and_probabilities(uint32_t tile, f32x16 (&next)[2], f32x16 (&s)[2], float scale_log2, uint32_t (&p)[16]) {
         constexpr int GROUPS = 2 * KS / 4, PAIRS = 16 / (2 * KS);               // pairs of probabilities behind each matrix instruction
-        const uint32_t at = tile + k_at;
+        uint32_t at = tile + k_at;
+        asm volatile("" : "+v"(at));                                            // (what follows from it is worked out here: kept for both tiles of a pair it takes registers)
         KFrag k[2];
         float sum[2] = {0.f, 0.f};
         __builtin_amdgcn_s_setprio(1);                                          // (ahead of the other wave's single products: 8192 tokens 1087 -> 1067 us)
@@ -226,7 +227,8 @@ struct AttnCore {
     // puts them where they are seen once everything else is done.
     template <bool MASKED>
     __device__ __forceinline__ void add_values(uint32_t tile, const uint32_t (&p)[16], uint32_t &odd) {
-        const uint32_t at[2] = {tile + v_at[0], tile + v_at[1]};
+        uint32_t at[2] = {tile + v_at[0], tile + v_at[1]};
+        asm volatile("" : "+v"(at[0]), "+v"(at[1]));
         VFrag v[2];
         v_read<0>(at, v[0]);
         core_for<0, CORE_KEYS / 16>([&](auto kk_) __attribute__((always_inline)) {

@@ -592,7 +592,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
         decode_k(kc, t + 1);
         load_v(t + 1, page, vc);
         load_k(t + 2, page_next, kc);
-        for (; t + 1 < c_end; t++) {
+        auto turn = [&](int t, f32x16 (&now)[2], f32x16 (&next)[2]) __attribute__((always_inline)) {
             meet();                                                             // V of tile t and K of t + 1 are there
             page = page_next;
             page_next = page_of(t + 3);
@@ -600,13 +600,20 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
             decode_k(kc, t + 2);
             load_v(t + 2, page, vc);
             load_k(t + 3, page_next, kc);
-            if (idle) continue;
-            f32x16 next[2];
-            core.scores_and_probabilities(k_tile(t + 1), next, s, a.scale_log2, p);
+            if (idle) return;
+            core.scores_and_probabilities(k_tile(t + 1), next, now, a.scale_log2, p);
             core.template add_values<false>(v_tile(t), p, odd);
+            if (t + 2 == n_c) mask(next, up_to(Lc - (t + 1) * CORE_KEYS));
+        };
+        f32x16 next[2];
+        for (; t + 2 < c_end; t += 2) {                                         // (two at a time: scores stay where they are)
+            turn(t, s, next);
+            turn(t + 1, next, s);
+        }
+        if (t + 1 < c_end) {
+            turn(t++, s, next);
             s[0] = next[0];
             s[1] = next[1];
-            if (t + 2 == n_c) mask(s, up_to(Lc - (t + 1) * CORE_KEYS));
         }
         meet();
         if (!idle) {
