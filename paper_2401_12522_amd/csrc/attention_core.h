@@ -224,7 +224,7 @@ struct AttnCore {
         return __builtin_bit_cast(bf16x8, make_uint4(p[4 * kk], p[4 * kk + 1], p[4 * kk + 2], p[4 * kk + 3]));
     }
     // o += V^T P^T of a tile.  MASKED: without V's infinities and NaN; whether there were any is noted in `odd`, and add_nonfinite
-    // puts them where they are seen once everything else is done.
+    // puts them where they are seen once everything else is done.  (They are looked for by the largest magnitude of 16 keys, two instructions a pair of values.)
     template <bool MASKED>
     __device__ __forceinline__ void add_values(uint32_t tile, const uint32_t (&p)[16], uint32_t &odd) {
         uint32_t at[2] = {tile + v_at[0], tile + v_at[1]};
@@ -235,12 +235,20 @@ struct AttnCore {
             constexpr int kk = decltype(kk_)::value;
             if constexpr (kk + 1 < CORE_KEYS / 16) v_read<kk + 1>(at, v[(kk + 1) & 1]);
             v_wait<(kk + 1 < CORE_KEYS / 16) ? 2 * NT : 0>(v[kk & 1]);
+            bf16x8 x[NT];
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
-                bf16x8 x = v_fragment(v[kk & 1], n);
-                if constexpr (MASKED) odd |= drop_nonfinite(x);
-                o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p_fragment(p, kk), o[n], 0, 0, 0);
+            for (int n = 0; n < NT; n++) x[n] = v_fragment(v[kk & 1], n);
+            if constexpr (MASKED) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int n = 0; n < NT; n++) top = largest_halves(top, x[n]);
+                if (__builtin_amdgcn_ballot_w64(nonfinite_halves(top) != 0) != 0) {
+#pragma unroll
+                    for (int n = 0; n < NT; n++) odd |= drop_nonfinite(x[n]);
+                }
             }
+#pragma unroll
+            for (int n = 0; n < NT; n++) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[n], p_fragment(p, kk), o[n], 0, 0, 0);
         });
     }
     // The infinities and NaN of up to 64 rows of V (row r at v + r * ld, the last one's number is `last`), seen where `seen` has the key's bit for this

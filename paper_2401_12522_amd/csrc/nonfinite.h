@@ -10,6 +10,15 @@ __device__ __forceinline__ bool has_nonfinite(bf16x8 v) {
     const uint4 u = __builtin_bit_cast(uint4, v);
     return (nonfinite_halves(u.x) | nonfinite_halves(u.y) | nonfinite_halves(u.z) | nonfinite_halves(u.w)) != 0;
 }
+// the larger magnitude bits of each half of m and of all pairs of v
+__device__ __forceinline__ uint32_t largest_halves(uint32_t m, bf16x8 v) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u4;
+    typedef __attribute__((ext_vector_type(2))) unsigned short h2;
+    const u4 x = __builtin_bit_cast(u4, v);
+#pragma unroll
+    for (int i = 0; i < 4; i++) m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(h2, m), __builtin_bit_cast(h2, x[i] & 0x7FFF7FFFu)));
+    return m;
+}
 // v without its infinities and NaN; not 0 if there were any
 __device__ __forceinline__ uint32_t drop_nonfinite(bf16x8 &v) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u4;

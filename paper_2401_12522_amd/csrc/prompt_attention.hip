@@ -184,7 +184,7 @@ __global__ __launch_bounds__(PA_WAVES * 64, HD == 64 ? 3 : 2) void prompt_attn_k
         }
         turn(t);
         mask(t, s);
-        core.probabilities(s, a.scale_log2, p, true);
+        core.probabilities(s, a.scale_log2, p, false);
         core.template add_values<true>(v_tile(t), p, odd);
         if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
             const int past = qi - t * CORE_KEYS;                                        // keys 0 .. past of the tile are seen
