@@ -48,6 +48,12 @@ __device__ __forceinline__ u32x4_t core_read_b128(uint32_t addr) {
     asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFFSET));
     return v;
 }
+// this lane's number, worked out where it is asked for: kept through a loop it takes a register
+__device__ __forceinline__ int core_lane() {
+    int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    asm volatile("" : "+v"(l));
+    return l;
+}
 template <int I, int N, typename F>
 __device__ __forceinline__ void core_for(F &&f) {
     if constexpr (I < N) {
@@ -250,6 +256,20 @@ struct AttnCore {
 #pragma unroll
             for (int n = 0; n < NT; n++) o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[n], p_fragment(p, kk), o[n], 0, 0, 0);
         });
+    }
+    // This lane's query's result o * scale as bf16, at dst (of its row).  The half waves (h) trade eights of columns, so that a lane writes 16 bytes.
+    __device__ __forceinline__ void put(uint16_t *dst, float scale, int h) const {
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                typedef __attribute__((ext_vector_type(2))) unsigned u2;
+                const u2 a = __builtin_amdgcn_permlane32_swap(core_pk_bf16(o[n][4 * i] * scale, o[n][4 * i + 1] * scale),
+                                                              core_pk_bf16(o[n][4 * i + 4] * scale, o[n][4 * i + 5] * scale), false, false);
+                const u2 b = __builtin_amdgcn_permlane32_swap(core_pk_bf16(o[n][4 * i + 2] * scale, o[n][4 * i + 3] * scale),
+                                                              core_pk_bf16(o[n][4 * i + 6] * scale, o[n][4 * i + 7] * scale), false, false);
+                *reinterpret_cast<uint4 *>(dst + 32 * n + 8 * (i + h)) = make_uint4(a[0], b[0], a[1], b[1]);
+            }
     }
     // The infinities and NaN of up to 64 rows of V (row r at v + r * ld, the last one's number is `last`), seen where `seen` has the key's bit for this
     // lane's query.  Rare, and slow: single values from memory.

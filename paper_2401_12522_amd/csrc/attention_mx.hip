@@ -513,12 +513,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
     const int nq = a.R * a.qpk;
     const bool idle = tile * AMW_ROWS + wave * 32 >= nq;                        // (it decodes all the same)
     // (what a lane is for, a query's row and its offsets, is worked out where it is used: kept through the loop, 8 bits of 128 spilled)
-    auto lane_now = [&]() __attribute__((always_inline)) {
-        int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-        asm volatile("" : "+v"(l));
-        return l;
-    };
-    auto query_now = [&]() __attribute__((always_inline)) { return min(tile * AMW_ROWS + wave * 32 + (lane_now() & 31), nq - 1); };
+    auto query_now = [&]() __attribute__((always_inline)) { return min(tile * AMW_ROWS + wave * 32 + (core_lane() & 31), nq - 1); };
 
     Core core;
     core.init(lane);
@@ -549,8 +544,8 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
         for (int s = 0; s < PARTS; s++) *(__attribute__((address_space(3))) u32x4_t *)(uintptr_t)(at ^ (16 * s)) = __builtin_bit_cast(u32x4_t, x[s]);
     };
     auto first_key = [&](int t) __attribute__((always_inline)) { return t * CORE_KEYS + 16 * wave; };
-    auto load_k = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.k, a.kv.k_scale, h, first_key(t), Lc, page, Keys::code_offset(lane_now()), Keys::scale_offset(lane_now())); };
-    auto load_v = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.v, a.kv.v_scale, h, first_key(t), Lc, page, Keys::code_offset(lane_now()), Keys::scale_offset(lane_now())); };
+    auto load_k = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.k, a.kv.k_scale, h, first_key(t), Lc, page, Keys::code_offset(core_lane()), Keys::scale_offset(core_lane())); };
+    auto load_v = [&](int t, int page, Keys &x) __attribute__((always_inline)) { x.load(a.kv, a.kv.v, a.kv.v_scale, h, first_key(t), Lc, page, Keys::code_offset(core_lane()), Keys::scale_offset(core_lane())); };
     auto page_of = [&](int t) __attribute__((always_inline)) { return Keys::page_of(a.kv, b, first_key(t), Lc); };
     auto decode = [&](const Keys &x, uint32_t tile, bool is_v) __attribute__((always_inline)) {
         bf16x8 v[PARTS];
@@ -561,7 +556,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
     auto decode_v = [&](const Keys &x, int t) __attribute__((always_inline)) { decode(x, v_tile(t), true); };
     // scores of keys that `sees` has no bit for: none
     auto mask = [&](f32x16 (&s)[2], uint64_t sees) __attribute__((always_inline)) {
-        sees >>= 4 * (lane_now() >> 5);
+        sees >>= 4 * (core_lane() >> 5);
 #pragma unroll
         for (int e = 0; e < 32; e++) {
             const uint32_t w = (uint32_t)(sees >> (e & 16 ? 32 : 0));
@@ -643,7 +638,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
         int n;
         uint64_t sees;
         rows_of(t, k, v, ldk, ldv, n, sees);
-        const int l = lane_now(), r = min(16 * wave + (l & 15), n - 1), first = VPL * (l >> 4);
+        const int l = core_lane(), r = min(16 * wave + (l & 15), n - 1), first = VPL * (l >> 4);
         bf16x8 x[PARTS], y[PARTS];
 #pragma unroll
         for (int i = 0; i < PARTS; i++) {
@@ -670,7 +665,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
             core.add_nonfinite(v, ldv, n - 1, sees);
         }
 
-    const int end_lane = lane_now(), qi = tile * AMW_ROWS + wave * 32 + (end_lane & 31), half = end_lane >> 5;
+    const int end_lane = core_lane(), qi = tile * AMW_ROWS + wave * 32 + (end_lane & 31), half = end_lane >> 5;
     if (qi >= nq) return;
     const AmxArgs z = amx_again();
     const int row = qi / z.qpk, head = h * z.qpk + (qi - row * z.qpk);
@@ -690,15 +685,14 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
         if (half == 0) *reinterpret_cast<float2 *>(z.part_ml + to * 2) = absent || l == 0.f ? make_float2(-INFINITY, 0.f) : make_float2(core.base + e, ldexpf(l, -e));
         return;
     }
+    // (an absent row gives zeros, and a sum of nothing)
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    uint16_t *dst = z.out + z.query(b, row, head) * HD + 4 * half;
+    uint16_t *dst = z.out + z.query(b, row, head) * HD;
+    core.put(dst, inv, half);
+    if (absent) {
 #pragma unroll
-    for (int n = 0; n < Core::NT; n++)
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) =
-                absent || l == 0.f ? make_uint2(0, 0) : make_uint2(core_pk_bf16(core.o[n][4 * i] * inv, core.o[n][4 * i + 1] * inv),
-                                                                  core_pk_bf16(core.o[n][4 * i + 2] * inv, core.o[n][4 * i + 3] * inv));
+        for (int i = 0; i < HD / 16; i++) *reinterpret_cast<uint4 *>(dst + 8 * (2 * i + half)) = make_uint4(0, 0, 0, 0);
+    }
 }
 
 // o = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max m): HD / 4 threads a query's columns, SIDE such rows of threads side by side its shares (and

@@ -92,7 +92,7 @@ __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &star
 template <int HD>
 __global__ __launch_bounds__(PA_WAVES * 64, HD == 64 ? 3 : 2) void prompt_attn_kernel(PromptArgs a) {
     using Core = AttnCore<HD>;
-    constexpr int KS = Core::KS, NT = Core::NT, TILE = Core::TILE, GPR = HD / 8, RPI = 64 / GPR;    // granules a row, rows a load instruction
+    constexpr int KS = Core::KS, TILE = Core::TILE, GPR = HD / 8, RPI = 64 / GPR;    // granules a row, rows a load instruction
     constexpr int LOADS = CORE_KEYS / RPI / PA_WAVES;                                   // load instructions of a wave, K or V tile
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];              // K tiles [2], V tiles [2]
     const int lane = threadIdx.x & 63, hf = lane >> 5, c = lane & 31;
@@ -193,15 +193,9 @@ __global__ __launch_bounds__(PA_WAVES * 64, HD == 64 ? 3 : 2) void prompt_attn_k
         t++;
     }
     for (; t < n_tiles; t++) turn(t);
-    if (qi >= len) return;
     const float inv = 1.0f / core_sum_halves(core.l_run);
-    uint16_t *dst = a.out + qrow * a.ldo + (int64_t)head * HD + 4 * hf;
-#pragma unroll
-    for (int n = 0; n < NT; n++)
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            *reinterpret_cast<uint2 *>(dst + 32 * n + 8 * i) = make_uint2(core_pk_bf16(core.o[n][4 * i] * inv, core.o[n][4 * i + 1] * inv),
-                                                                          core_pk_bf16(core.o[n][4 * i + 2] * inv, core.o[n][4 * i + 3] * inv));
+    const int end_lane = core_lane(), query = q0 + (end_lane & 31);
+    if (query < len) core.put(a.out + (int64_t)(start + query) * a.ldo + (int64_t)head * HD, inv, end_lane >> 5);
 }
 
 extern "C" int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_head_stride, const void *d_k, int64_t ldk, int64_t k_head_stride,
