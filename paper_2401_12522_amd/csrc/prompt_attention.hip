@@ -131,8 +131,8 @@ __global__ __launch_bounds__(PA_WAVES * 64, HD == 64 ? 3 : 2) void prompt_attn_k
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(dst + i * 1024), 16,
                                                      is_v ? (v_col ^ (16 * V_STEP * i)) + v_row : (k_col ^ (16 * K_STEP * i)) + k_row, (R0 * wave + RPI * i) * ld, 0, 0);
     };
-    auto landed = [&]() __attribute__((always_inline)) {                                // everyone's loads are in LDS, everyone's reads are done
-        __builtin_amdgcn_s_waitcnt(0x0070);                                             // vmcnt(0), lgkmcnt(0)
+    auto landed = [&](auto behind) __attribute__((always_inline)) {                     // everyone's loads but the last few are in LDS, everyone's reads are done
+        __builtin_amdgcn_s_waitcnt(0x0070 + decltype(behind)::value);                   // vmcnt(behind), lgkmcnt(0)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(PA_WAVES * 64, HD == 64 ? 3 : 2) void prompt_attn_k
     };
 
     auto turn = [&](int t) __attribute__((always_inline)) {                             // tile t's V and t + 1's K are there; the next are asked for
-        landed();
+        landed(std::integral_constant<int, 0>{});
         if (t + 2 < n_tiles) fetch(t + 2, false);
         if (t + 1 < n_tiles) fetch(t + 1, true);
     };
@@ -159,10 +159,15 @@ __global__ __launch_bounds__(PA_WAVES * 64, HD == 64 ? 3 : 2) void prompt_attn_k
     f32x16 s[2];
     uint32_t p[16], odd = 0;
     int t = 0;
+    static_assert(2 * LOADS < 16, "the count of a wait");
+    asm volatile("" ::: "memory");                                                      // (the queries are asked for before the tiles: the wait below counts what is behind K's first)
+    __builtin_amdgcn_sched_barrier(0);
     fetch(0, false);
     fetch(0, true);
-    if (n_tiles > 1) fetch(1, false);
-    landed();
+    if (n_tiles > 1) {
+        fetch(1, false);
+        landed(std::integral_constant<int, 2 * LOADS>{});
+    } else landed(std::integral_constant<int, LOADS>{});
     if (q0 < len) {
         core.scores(k_tile(0), s);
         if (n_whole == 0) mask(0, s);
