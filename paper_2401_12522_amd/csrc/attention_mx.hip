@@ -495,8 +495,8 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
 // Many queries a K/V head (a tree under grouped heads): a workgroup's waves own 32 queries each and share the keys, in tiles of 64 that they decode
 // together into LDS, each wave 16 rows, a tile ahead of the products (attention_core.h).  Scores run a tile ahead of the values too, so
 // K is decoded two tiles ahead and V one, from codes that were asked for a tile earlier.  A wave finishes its own queries.  Bound by exponentials, conversions and
-// matrix instructions together: a turn of two workgroups on a CU is 2.43 us, 884 TFLOP/s over the card (with one 1.56); four trees of 68 rows over 1024 to 4096 keys of 8 bits, 64/8
-// heads, 52 us, and 6.5 for the shares' sum.
+// matrix instructions together: a turn of two workgroups on a CU is 2.1 us, 1020 TFLOP/s over the card (with one 1.37); four trees of 68 rows over 1024 to 4096 keys of 8 bits, 64/8
+// heads, 50.6 us, and 6.3 for the shares' sum.
 #define AMW_ROWS (32 * AMX_WAVES)
 
 template <int HD, int BITS>
@@ -697,7 +697,7 @@ __global__ __launch_bounds__(AMX_WAVES * 64, 2) void attn_mx_wide_kernel(AmxArgs
 
 // o = sum_s w_s o_s / sum_s w_s l_s, w_s = 2^(m_s - max m): HD / 4 threads a query's columns, SIDE such rows of threads side by side its shares (and
 // in a workgroup of 256 or more threads as many queries as there is room for).  A share without keys for the query has m = -inf and is left out
-// (nothing of it need have been written).  Bound by what the shares left in memory: 12 shares of 4352 queries 6.5 us, 27 MB; few of them: by a launch and two ways to memory, 4.1.
+// (nothing of it need have been written).  Bound by what the shares left in memory: 12 shares of 4352 queries 6.3 us, 27 MB; few of them: by a launch and two ways to memory, 4.1.
 template <int HD, int SIDE, int THREADS>
 __global__ __launch_bounds__(THREADS) void attn_mx_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, const int2 *__restrict__ share_of, int64_t n_queries,
                                                                 int of_sequence, int stride, int n_shares, uint16_t *__restrict__ out) {
@@ -781,17 +781,17 @@ struct AmxPlan { bool wide; int tiles_u, waves, n_tiles, shares, per_share; int6
 //   than a CU takes codes in, 35 KB a us; the bytes that all of them read at 6 TB/s, 5 where tiles of queries read the same ones again (of these two the longer, and a
 //   quarter of the other); and, where the keys are split, a second kernel and what the shares write and read, at 4.5 TB/s.
 // Split launches fill the card once.  A batch's lengths are taken to be half to three quarters of the hint on average; not split, its longest decides.
-// Measured (16 queries in 4 waves / 32 / wide): a turn with one workgroup a CU 0.9 / 1.25 / 1.56 us, with two 1.44 / 2.1 / 2.43; the start and end 5.6 / 5.6 / 7; a turn of
+// Measured (16 queries in 4 waves / 32 / wide): a turn with one workgroup a CU 0.9 / 1.25 / 1.37 us, with two 1.44 / 2.1 / 2.1; the start and end 5.6 / 5.6 / 7; a turn of
 // 8 waves 1.0.  Each kind with its best shares, 16 queries in 8 waves / in 4 / 32 / wide:
-//   68 rows, 32 heads of their own keys, 1024 keys of 4 bits 12.0 / 14.4 / 16.1 / 20.1 us; 4096 keys of 8 bits 43 / 41 / 30 / 25; four sequences of 400 to 1100
-//   keys 31.9 / 21.7 / 30.8 / 32.1; 4 sequences of 1024 to 4096 keys, 64/8 heads 146 / 127 / 83 / 56; 20 rows there 39 / 32 / 31 / 34; single tokens: 32 sequences
+//   68 rows, 32 heads of their own keys, 1024 keys of 4 bits 11.9 / 14.3 / 15.9 / 19.4 us; 4096 keys of 8 bits 42 / 40 / 30 / 25; four sequences of 400 to 1100
+//   keys 31.7 / 21.5 / 29.1 / 29.3; 4 sequences of 1024 to 4096 keys, 64/8 heads 146 / 127 / 82 / 54; 20 rows there 39 / 32 / 30 / 32; single tokens: 32 sequences
 //   of up to 8192 keys 42 / 33.4 / 44 / 67; one of 131072 keys of 4 bits 32 / 37 / 42 / 62; one of 1000, 32 heads 10.2 / 10.2 / 10.6 / 12 (the last three with
 //   a second kernel, whose launch costs the host as much again: hence 3.5 us for it, more than its own time).
 // With shares cut from the hint instead, 8 sequences of 100 to 4000 keys of 8 bits, 32 heads, took 43 us (now 29), 3 of 0 to 39168, 6/2 heads 28 (17), 30 of 0 to
 // 26000 45 (37), the 32 above 36.
 static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int bits, int ctx_hint, int n_prompt) {
     static const struct { int queries, unit, waves, slots; double start, one, many; } kinds[4] = {
-        {16, AMX_CHUNK, 8, 256, 5.6, 1.0, 1.0}, {16, AMX_CHUNK, 4, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, 4, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 4, 512, 7.0, 1.56, 2.43}};
+        {16, AMX_CHUNK, 8, 256, 5.6, 1.0, 1.0}, {16, AMX_CHUNK, 4, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, 4, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 4, 512, 7.0, 1.37, 2.1}};
     static const int per_sequence[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128, 192, 256};
     const int64_t nq = (int64_t)rows * (Hq / Hkv);
     const double size = hd / 128.0, key_bytes = 2 * (hd * bits / 8 + hd / 32), cache = (double)batch * Hkv * ctx_hint * (batch > 1 ? 0.5 : 1.0) * key_bytes;

@@ -9,9 +9,9 @@
 //    the values, V one: scores run a tile ahead); one barrier a tile.  Rows are swizzled by 16-byte columns on the way (by where a lane fetches from: LDS takes them in lane order),
 //    K is read back by rows, V by transposed reads.
 //  * Key tiles before a wave's queries need no mask.  Workgroups start with the longest walks.
-// Bound by matrix instructions at the clock that the card holds under them, with the exponentials between them: 8192 tokens of 64/8 heads of 128 1019 us, 1080 TFLOP/s
-// of what the mask leaves, 0.90 of the library's rate for a product of 8192^3; a turn of two workgroups on a CU 1.96 us.  Ragged prompts by the packing of their walks: 2049, 1411, 977,
-// 350 tokens and less of 32 heads 90 us, 74 of them a packing without starts and ends.
+// Bound by matrix instructions at the clock that the card holds under them, with the exponentials between them: 8192 tokens of 64/8 heads of 128 1013 us, 1085 TFLOP/s
+// of what the mask leaves, 0.91 of the library's rate for a product of 8192^3; a turn of two workgroups on a CU 1.95 us.  Ragged prompts by the packing of their walks: 2049, 1411, 977,
+// 350 tokens and less of 32 heads 82 us, 74 of them a packing without starts and ends.
 #include <cmath>
 #include <type_traits>
 #include "attention_core.h"
@@ -88,7 +88,7 @@ __device__ __forceinline__ bool pa_find(const PromptArgs &a, int tile, int &star
     return false;
 }
 
-// (of narrow heads a CU holds three workgroups: 8192 tokens of 64/8 heads of 64 in 590 us, with two 616; nine packed prompts of 32 heads 51, with two 54.7)
+// (of narrow heads a CU holds three workgroups: 8192 tokens of 64/8 heads of 64 in 590 us, with two 616, when both were timed, now 583; nine packed prompts of 32 heads 51, with two 54.7, now 46.5)
 template <int HD>
 __global__ __launch_bounds__(PA_WAVES * 64, HD == 64 ? 3 : 2) void prompt_attn_kernel(PromptArgs a) {
     using Core = AttnCore<HD>;
