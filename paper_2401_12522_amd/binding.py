@@ -850,7 +850,8 @@ def qk_norm_rope(x, pos, cos, sin, n_heads, n_kv_heads, q_gain=None, k_gain=None
     L, dev = _lib or lib(), torch.cuda.current_device()
     max_pos, half = table = _shape("cos", cos, 2)
     hd, bf16 = 2 * half, torch.bfloat16
-    m, _, ldx = _matrix("x", x, _F32_BF16, dev, None, (n_heads + 2 * n_kv_heads) * hd)
+    m = _shape("x", x, 2)[0]
+    ldx = _strides("x", x, _F32_BF16, dev, (m, (n_heads + 2 * n_kv_heads) * hd))[0]
     dtype, pqg, pkg, pv, ldv, hv = x.dtype, 0, 0, 0, 0, 0
     if q_gain is not None:
         pqg = _dense("q_gain", q_gain, _BF16, dev, (hd,))

@@ -113,3 +113,7 @@ def test_empty_calls():
     k = torch.zeros((1, 2, 0, 64), device="cuda")
     bita.kv_read_mx(cache, k, k, i32([3]))
     assert torch.equal(cache.k, before)
+    x = torch.zeros((0, 8 * 64), device="cuda")
+    cos = torch.ones(9, 32, device="cuda")
+    q, k, v = bita.qk_norm_rope(x, i32([]), cos, cos, 4, 2)
+    assert q.shape == (0, 4, 64) and k.shape == v.shape == (0, 2, 64)

@@ -274,6 +274,8 @@ CUTS = [
     (17, 68, 4, 64, 2, 64, [40, 39, 31, 0, 1, 33, 32, 17, 40, 5, 6, 7, 8, 9, 10, 11, 12], 16, 3),
     (1, 130, 5, 16, 1, 128, [6000], 256, 16),
     (3, 130, 5, 16, 1, 128, [2000, 0, 900], 256, 70),
+    (66, 16, 2, 16, 1, 64, [(211 * i) % 1801 for i in range(66)], 16, 3),
+    (1, 512, 4, 2, 1, 64, [200], 0, 100),                         # the most rows, a prefix of two tiles
 ]
 
 
@@ -347,4 +349,23 @@ def test_a_block_that_is_no_number_in_every_cut(bits, n, R, masks, hq, hkv, hd, 
     group = hq // hkv
     assert torch.isnan(got[b, :, :group, 32:64]).all()
     got[b, :, :group, 32:64] = out[b, :, :group, 32:64]
+    near(got, out, tol)
+
+
+@BITS
+@pytest.mark.parametrize("n,R,masks,hq,hkv,hd,ctx,page,P", [c for c in CUTS if c[1] > 4])
+def test_absent_rows_in_every_cut(bits, n, R, masks, hq, hkv, hd, ctx, page, P):
+    """Zeros for tree rows without a token, also where a NaN in their query would show; mask rows are never absent."""
+    call, (out, tol), (cache, q, *_) = case(n, R, masks, hq, hkv, hd, bits, ctx, page, P, seed=11)
+    token = torch.arange(n * R, dtype=torch.int32).view(n, R)
+    gone = torch.zeros(n, R, dtype=torch.bool)
+    gone[:, [1, 3, R - masks - 1]] = True
+    gone[0, 2] = n > 1
+    gone[:, R - masks:] = False
+    token[gone] = -5
+    token[:, R - masks:] = -1
+    q[gone] = float("nan")
+    got = call(token=token.cuda()).cpu().double().view(out.shape)
+    assert (got[gone] == 0).all() and not torch.signbit(got[gone]).any()
+    got[gone] = out[gone]
     near(got, out, tol)
