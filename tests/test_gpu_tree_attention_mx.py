@@ -369,3 +369,13 @@ def test_absent_rows_in_every_cut(bits, n, R, masks, hq, hkv, hd, ctx, page, P):
     assert (got[gone] == 0).all() and not torch.signbit(got[gone]).any()
     got[gone] = out[gone]
     near(got, out, tol)
+
+
+def test_more_sequences_than_a_wave_has_lanes_in_wide_shares():
+    """A large batch is cut by the hint: sequences with fewer shares than the longest, and with one."""
+    n, R, ctx = 65, 16, [(53 * i) % 4001 for i in range(64)] + [4000]
+    assert cut_of(8, n, R, 2, 8, 1, 64, ctx, 64, 3) == (128, 4, True)
+    call, (out, tol), _ = case(n, R, 2, 8, 1, 64, 8, ctx, 64, 3, seed=13)
+    got = call()
+    near(got, out, tol)
+    assert torch.equal(call(), got)
