@@ -12,8 +12,8 @@
 //    B operand of O^T = V^T P^T if that product takes the keys in the same order: probabilities stay in registers.
 //  * V^T needs eight keys of one column in a lane: V goes to LDS as bf16 rows and comes back by transposed reads.  The region is the wave's own,
 //    and its LDS instructions run in order, so there is no barrier in the loop.
-// Bound by what a CU takes in at low batch (one sequence of 131072 keys, 64/8 heads, 4 bits: 143 MB in 28 us, 5.1 TB/s, and a merge of 4), by its own start and end at
-// short lengths (1000 keys, 32 heads: 10 us for 4.4 MB), by the conversions and the exponentials between, where a K/V head has many queries by matrix instructions.
+// Bound by what a CU takes in at low batch (one sequence of 131072 keys, 64/8 heads, 4 bits: 143 MB in 26.6 us, 5.4 TB/s, and a merge of 4), by its own start and end at
+// short lengths (1000 keys, 32 heads: 9.8 us for 4.4 MB), by the conversions and the exponentials between, where a K/V head has many queries by matrix instructions.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -801,7 +801,7 @@ struct AmxPlan { bool wide; int tiles_u, waves, n_tiles, shares, per_share; int6
 // 8 waves 1.0.  Each kind with its best shares, 16 queries in 8 waves / in 4 / 32 / wide:
 //   68 rows, 32 heads of their own keys, 1024 keys of 4 bits 11.9 / 14.3 / 15.9 / 19.4 us; 4096 keys of 8 bits 42 / 40 / 30 / 25; four sequences of 400 to 1100
 //   keys 31.7 / 21.5 / 29.1 / 29.3; 4 sequences of 1024 to 4096 keys, 64/8 heads 146 / 127 / 82 / 54; 20 rows there 39 / 32 / 30 / 32; single tokens: 32 sequences
-//   of up to 8192 keys 42 / 33.4 / 44 / 67; one of 131072 keys of 4 bits 32 / 37 / 42 / 62; one of 1000, 32 heads 10.2 / 10.2 / 10.6 / 12 (the last three with
+//   of up to 8192 keys 42 / 32.5 / 44 / 67; one of 131072 keys of 4 bits 31 / 37 / 42 / 62; one of 1000, 32 heads 9.8 / 10.0 / 10.6 / 12 (the last three with
 //   a second kernel, whose launch costs the host as much again: hence 3.5 us for it, more than its own time).
 // With shares cut from the hint instead, 8 sequences of 100 to 4000 keys of 8 bits, 32 heads, took 43 us (now 29), 3 of 0 to 39168, 6/2 heads 28 (17), 30 of 0 to
 // 26000 45 (37), the 32 above 36.
