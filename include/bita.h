@@ -444,7 +444,7 @@ int bita_qk_norm_rope(const void *d_x, int32_t x_type, int32_t m_rows, int64_t l
  *   d_prompt_k, d_prompt_v  bf16 [n_kv_heads][n_prompt][hd] or NULL with n_prompt 0
  *   d_ctx_len [B] (read as at most ctx_hint and smax);  ctx_hint: HOST upper bound of them, at most smax (2^30).  It decides the launch and the
  *          workspace; which keys a workgroup takes follows from the lengths themselves (up to 64 sequences), so that a graph captured for long
- *          sequences keeps the card busy over short ones
+ *          sequences spreads shorter ones over the card too
  *   d_token   [B][R] or NULL: a tree row with a negative token is absent and its output zero (it stays visible to the rows below it)
  *   d_out  bf16 [B][R][n_heads * hd];  d_ws: bita_tree_attention_mx_workspace_bytes(), a multiple of 16, nothing in it kept from call to call, calls that
  *          may run at the same time have each their own.  The pointers of bf16 tensors are multiples of 16 bytes.
