@@ -497,7 +497,9 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
             if (at.split) {
                 const int64_t to = z.part(at.share, row, head);
                 *reinterpret_cast<float4 *>(z.part_o + to * HD + 16 * n + 4 * g) = x;
-                if (n == 0 && g == 0) *reinterpret_cast<float2 *>(z.part_ml + to * 2) = absent ? make_float2(-INFINITY, 0.f) : make_float2(m_tot[u], l_tot[u]);
+                // (-inf says that there was nothing to sum: where no score was a number the sum is NaN and its reference any number, so that the sum over shares has it)
+                const float ref = absent ? -INFINITY : m_tot[u] == -INFINITY && l_tot[u] != 0.f ? 0.f : m_tot[u];
+                if (n == 0 && g == 0) *reinterpret_cast<float2 *>(z.part_ml + to * 2) = make_float2(ref, absent ? 0.f : l_tot[u]);
                 continue;
             }
             // (a NaN sum stays one; a sum of nothing, or an absent row, gives zeros)
