@@ -449,7 +449,8 @@ int bita_qk_norm_rope(const void *d_x, int32_t x_type, int32_t m_rows, int64_t l
  *   d_out  bf16 [B][R][n_heads * hd];  d_ws: bita_tree_attention_mx_workspace_bytes(), a multiple of 16, nothing in it kept from call to call, calls that
  *          may run at the same time have each their own.  The pointers of bf16 tensors are multiples of 16 bytes.
  * Any n_heads that is a multiple of n_kv_heads; batch * n_heads at most 2^17, n_prompt at most 2^20.  One kernel, or two where the keys are split; may be captured.  Scores, sums and
- * accumulation are fp32; probabilities go to the matrix product as bf16.
+ * accumulation are fp32; probabilities go to the matrix product as bf16.  Weighted values are summed before they are divided by the weights' sum: results are finite
+ * where the largest finite |v| is at most 2^108 / (keys that a query sees).
  * bita_tree_attention_mx_plan_info: how it is cut (for tests and reports): out4 (HOST) = {shares that a sequence's keys are
  * split into, on average and rounded up, queries of a workgroup, waves of a workgroup, workgroups}. */
 size_t bita_tree_attention_mx_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t bits,
@@ -468,7 +469,8 @@ int bita_tree_attention_mx(const bita_tree_template *t, const void *d_q, const b
  *   d_cu_seqlens   [n_seqs + 1], device, not decreasing, between 0 and n_tokens (clamped; sequences may be empty)
  *   d_out          bf16 rows of n_heads * head_dim, ldo apart; rows outside all sequences are left as they are
  * head_dim 64 or 128, any n_heads that is a multiple of n_kv_heads; rows of k and of v at most 2^24 elements apart.  Scores, sums and accumulation
- * are fp32; probabilities go to the matrix product as bf16.  One kernel; may be captured. */
+ * are fp32; probabilities go to the matrix product as bf16, and results are finite where the largest finite |v| is at most 2^108 / (keys that a query sees).  One
+ * kernel; may be captured. */
 int bita_prompt_attention(const void *d_q, int64_t ldq, int64_t q_head_stride, const void *d_k, int64_t ldk, int64_t k_head_stride, const void *d_v,
                           int64_t ldv, int64_t v_head_stride, const int32_t *d_cu_seqlens, int32_t n_seqs, int32_t n_tokens, int32_t n_heads,
                           int32_t n_kv_heads, int32_t head_dim, void *d_out, int64_t ldo, void *stream);

@@ -16,6 +16,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 
 #define CORE_KEYS 64
+#define CORE_SUM 0x1p24f                // the largest sum of a lane's 32 probabilities of a tile that leaves their reference where it is (of a true maximum: 2^5)
 
 __device__ __forceinline__ float core_exp2(float x) { return __builtin_amdgcn_exp2f(x); }       // results below 2^-126 are zero
 __device__ __forceinline__ uint32_t core_pk_bf16(float a, float b) {
@@ -124,7 +125,7 @@ struct AttnCore {
     __device__ __forceinline__ void take_maximum(float mx, float scale_log2) {
         if (__builtin_amdgcn_ballot_w64(mx > m_run) != 0) {
             const float m_new = fmaxf(m_run, core_max_halves(mx));
-            // in two halves: what is rescaled may be up to 2^60 (probabilities), and one factor below 2^-126 would be 0
+            // in two halves: what is rescaled may be far above 1, and one factor below 2^-126 would be 0
             const float alpha = m_new == -INFINITY ? 1.f : core_exp2((m_run - m_new) * (0.5f * scale_log2));
             m_run = m_new;
             base = m_new == -INFINITY ? 0.f : m_new * scale_log2;
@@ -149,9 +150,12 @@ struct AttnCore {
         }
         return sum[0] + sum[1];
     }
-    // The reference `base` need not be the maximum: bf16 and fp32 have one range of exponents, so a probability above 1 loses nothing, and the tile's
-    // maximum is looked for (look) only where the reference is not a true maximum yet, or before a sum leaves that range.  (Nothing above
+    // The reference `base` need not be the maximum: bf16 and fp32 have one range of exponents, so a probability above 1 loses nothing by itself, and the tile's
+    // maximum is looked for (look) only where the reference is not a true maximum yet, or before a sum passes CORE_SUM.  (Nothing above
     // 2^-126 of the largest is lost; a query that has met nothing but zeros is looked at again.)
+    // The products with V share that range: n keys have a sum of up to 2^19 n, so values are finite on the way up to max |v| = 2^108 / n (with the true maximum, 2^127 / n).  What the limit
+    // costs where scores spread widely, by 1, 3 and 10 nats: 8192 tokens 982, 1002, 1070 us, four trees of 68 rows 54, 52.4, 61; with 2^16 983, 1015, 1097 and 54, 53.3, 66, with 2^6
+    // 1004, 1096, 1180 and 55, 63, 70; with 2^60, where values of 2^68 overflowed, 984, 1001, 1006 and 54, 52.5, 53.
     __device__ __forceinline__ void probabilities(f32x16 (&s)[2], float scale_log2, uint32_t (&p)[16], bool look) {
         float sum;
         for (;;) {
@@ -160,7 +164,7 @@ struct AttnCore {
                 take_maximum(largest(s), scale_log2);
             }
             sum = exponentials(s, scale_log2, p);
-            if (look || __builtin_amdgcn_ballot_w64(sum > 0x1p60f || l_run + sum == 0.f) == 0) break;
+            if (look || __builtin_amdgcn_ballot_w64(sum > CORE_SUM || l_run + sum == 0.f) == 0) break;
             look = true;
         }
         l_run += sum;
@@ -196,7 +200,7 @@ struct AttnCore {
         });
         __builtin_amdgcn_s_setprio(0);
         float total = sum[0] + sum[1];
-        if (__builtin_amdgcn_ballot_w64(total > 0x1p60f || l_run + total == 0.f) != 0) {
+        if (__builtin_amdgcn_ballot_w64(total > CORE_SUM || l_run + total == 0.f) != 0) {
             asm volatile("" : "+v"(s[0]), "+v"(s[1]));                          // (else the maximum is taken of every tile, ahead of time)
             take_maximum(largest(s), scale_log2);
             total = exponentials(s, scale_log2, p);
