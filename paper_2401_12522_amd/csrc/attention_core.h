@@ -151,8 +151,8 @@ struct AttnCore {
         return sum[0] + sum[1];
     }
     // The reference `base` need not be the maximum: bf16 and fp32 have one range of exponents, so a probability above 1 loses nothing by itself, and the tile's
-    // maximum is looked for (look) only where the reference is not a true maximum yet, or before a sum passes CORE_SUM.  (Nothing above
-    // 2^-126 of the largest is lost; a query that has met nothing but zeros is looked at again.)
+    // maximum is looked for (look) only before a sum passes CORE_SUM, or while there is no maximum: a query whose scores were all -inf has no reference, and what
+    // it summed without one would be dropped with the first that it gets.  (Nothing above 2^-126 of the largest is lost.)
     // The products with V share that range: n keys have a sum of up to 2^19 n, so values are finite on the way up to max |v| = 2^108 / n (with the true maximum, 2^127 / n).  What the limit
     // costs where scores spread widely, by 1, 3 and 10 nats: 8192 tokens 982, 1002, 1070 us, four trees of 68 rows 54, 52.4, 61; with 2^16 983, 1015, 1097 and 54, 53.3, 66, with 2^6
     // 1004, 1096, 1180 and 55, 63, 70; with 2^60, where values of 2^68 overflowed, 984, 1001, 1006 and 54, 52.5, 53.
@@ -164,7 +164,7 @@ struct AttnCore {
                 take_maximum(largest(s), scale_log2);
             }
             sum = exponentials(s, scale_log2, p);
-            if (look || __builtin_amdgcn_ballot_w64(sum > CORE_SUM || l_run + sum == 0.f) == 0) break;
+            if (look || __builtin_amdgcn_ballot_w64(sum > CORE_SUM || m_run == -INFINITY) == 0) break;
             look = true;
         }
         l_run += sum;
@@ -200,7 +200,7 @@ struct AttnCore {
         });
         __builtin_amdgcn_s_setprio(0);
         float total = sum[0] + sum[1];
-        if (__builtin_amdgcn_ballot_w64(total > CORE_SUM || l_run + total == 0.f) != 0) {
+        if (__builtin_amdgcn_ballot_w64(total > CORE_SUM || m_run == -INFINITY) != 0) {
             asm volatile("" : "+v"(s[0]), "+v"(s[1]));                          // (else the maximum is taken of every tile, ahead of time)
             take_maximum(largest(s), scale_log2);
             total = exponentials(s, scale_log2, p);
