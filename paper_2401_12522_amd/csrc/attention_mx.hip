@@ -797,8 +797,12 @@ struct AmxPlan { bool wide; int tiles_u, waves, n_tiles, shares, per_share; int6
 // keys of all sequences are split into (as many as sequences: not at all).  The estimate behind the choice, in us at head_dim 128:
 //   a round of workgroups: their start and end, and their turns (256 keys, 128, 128, 64) at the pace of one workgroup a CU or of as many as a CU holds, but no faster
 //   than a CU takes codes in, 35 KB a us; the bytes that all of them read at 6 TB/s, 5 where tiles of queries read the same ones again (of these two the longer, and a
-//   quarter of the other); and, where the keys are split, a second kernel and what the shares write and read, at 4.5 TB/s.
-// Split launches fill the card once.  A batch's lengths are taken to be half to three quarters of the hint on average; not split, its longest decides.
+//   quarter of the other); and, where the keys are split, a second kernel and what the shares write and read, at 9 TB/s (it is still in a cache: 12 shares of 4352 queries 6 us).
+// Split launches fill the card once (three workgroups of 16 queries and 4 waves a CU; of 8 bits at head_dim 128 a CU holds two, but shares cut for two were no better).
+// A batch's lengths are taken to be half to three quarters of the hint on average; not split, its longest decides.  Where sequences are alike instead, amx_place, whose
+// shares have one size, gives each as many as fit for all and leaves the rest empty (17 sequences and 32 shares: one each); what that costs more counts for three tenths.
+// Without that, equal lengths: 17 sequences of 8192 keys, 64/8 heads, 46 us at 4 bits and 78 at 8 (now 35 and 59), 33 at 8 bits 164 (138), four trees of 68 rows over 3000 keys 80
+// (51), of 5 sequences of 4096, 32/32 heads, 8 bits 43 (36); what it took where lengths differ: 33 sequences of 8 bits 66 (77), 8 of 4096, 32/32 heads 23 (26), most others nothing.
 // Measured (16 queries in 4 waves / 32 / wide): a turn with one workgroup a CU 0.9 / 1.25 / 1.37 us, with two 1.44 / 2.1 / 2.1; the start and end 5.6 / 5.6 / 7; a turn of
 // 8 waves 1.0.  Each kind with its best shares, 16 queries in 8 waves / in 4 / 32 / wide:
 //   68 rows, 32 heads of their own keys, 1024 keys of 4 bits 11.9 / 14.3 / 15.9 / 19.4 us; 4096 keys of 8 bits 42 / 40 / 30 / 25; four sequences of 400 to 1100
@@ -812,7 +816,7 @@ static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int bits, 
         {16, AMX_CHUNK, 8, 256, 5.6, 1.0, 1.0}, {16, AMX_CHUNK, 4, 768, 5.6, 0.9, 1.44}, {32, AMX_CHUNK, 4, 512, 5.6, 1.25, 2.1}, {AMW_ROWS, CORE_KEYS, 4, 512, 7.0, 1.37, 2.1}};
     static const int per_sequence[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 80, 96, 128, 192, 256};
     const int64_t nq = (int64_t)rows * (Hq / Hkv);
-    const double size = hd / 128.0, key_bytes = 2 * (hd * bits / 8 + hd / 32), cache = (double)batch * Hkv * ctx_hint * (batch > 1 ? 0.5 : 1.0) * key_bytes;
+    const double size = hd / 128.0, key_bytes = 2 * (hd * bits / 8 + hd / 32), keys = (double)batch * Hkv * ctx_hint * key_bytes;
     AmxPlan p = {};
     double best = 1e300;
     for (int k = 0; k < (nq <= 16 ? 2 : nq <= 32 ? 3 : 4); k++) {
@@ -822,18 +826,29 @@ static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int bits, 
         auto units = [&](int64_t n) { return (n + kind.unit - 1) / kind.unit; };
         auto turns_of = [&](int64_t n) { return (units(n_prompt) + units(n) + units(rows) + unroll - 1) / unroll; };
         const int64_t longest = turns_of(ctx_hint), usual = turns_of(batch > 1 ? (int64_t)(0.6 * ctx_hint) : ctx_hint), share_wgs = (int64_t)Hkv * n_tiles;
-        auto consider = [&](int64_t shares, int64_t per) {
+        // of sequences that are alike, all as long as the hint, or of lengths that differ
+        auto estimate = [&](int64_t shares, int64_t per, bool alike) {
             const bool split = shares > batch;
-            const int64_t wgs = shares * share_wgs;
-            const double turns = !split ? (double)longest : batch > 64 ? (double)per : (double)(usual * batch + shares - 1) / shares + (batch > 1 ? 0.5 : 0.0);
+            double turns = (double)longest, wgs = (double)shares * share_wgs;
+            if (split && batch > 64) turns = (double)per;
+            else if (split && alike) {                                          // every sequence has as many shares, and the rest has nothing to do
+                const int64_t p = (longest + shares / batch - 1) / (shares / batch);
+                turns = (double)p;
+                wgs = (double)((longest + p - 1) / p * batch * share_wgs);
+            } else if (split) turns = (double)(usual * batch + shares - 1) / shares + (batch > 1 ? 0.5 : 0.0);
             // (not split, a batch's short sequences leave room for others; alone on a CU, a workgroup leaves it to the next one late)
-            const double busy = (double)wgs * (k && batch > 1 && (!split || batch > 64) ? 0.75 : 1.0);
-            const double rounds = k && batch > 1 ? std::max(busy / kind.slots, 1.0) : (double)((wgs + kind.slots - 1) / kind.slots);
-            const double on_a_cu = std::min(busy < 256 ? 1.0 : busy / 256, kind.slots / 256.0);
+            const double busy = wgs * (k && batch > 1 && !alike && (!split || batch > 64) ? 0.75 : 1.0);
+            const double rounds = k && batch > 1 ? std::max(busy / kind.slots, 1.0) : std::ceil(wgs / kind.slots);
+            const double on_a_cu = std::min(std::max(split && batch <= 64 ? std::ceil(busy / 256) : busy / 256, 1.0), kind.slots / 256.0);
             const double turn = std::max(size * (busy <= 256 ? kind.one : kind.many), on_a_cu * unroll * kind.unit * key_bytes / 35e3);
-            const double pace = rounds * turns * turn, load = cache * n_tiles / (n_tiles > 1 ? 5e6 : 6e6);
+            const double pace = rounds * turns * turn, load = keys * (batch > 1 && !alike ? 0.5 : 1.0) * n_tiles / (n_tiles > 1 ? 5e6 : 6e6);
             double us = rounds * kind.start + std::max(pace, load) + 0.25 * std::min(pace, load);
-            if (split) us += 3.5 + 0.03 * (double)shares / batch + (double)shares * rows * Hq * hd * 8 / 4.5e6;
+            if (split) us += 3.5 + 0.03 * (double)shares / batch + (double)shares * rows * Hq * hd * 8 / 9e6;
+            return us;
+        };
+        auto consider = [&](int64_t shares, int64_t per) {
+            double us = estimate(shares, per, false);
+            if (batch > 1 && batch <= 64) us += 0.3 * std::max(estimate(shares, per, true) - us, 0.0);
             if (us < best) {
                 best = us;
                 p.wide = k == 3;
@@ -842,7 +857,7 @@ static AmxPlan amx_plan(int batch, int rows, int Hq, int Hkv, int hd, int bits, 
                 p.n_tiles = n_tiles;
                 p.shares = (int)shares;
                 p.per_share = (int)per;
-                p.workgroups = wgs;
+                p.workgroups = shares * share_wgs;
             }
         };
         for (int want : per_sequence) {
