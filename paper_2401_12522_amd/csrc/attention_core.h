@@ -17,6 +17,7 @@ typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 
 #define CORE_KEYS 64
 #define CORE_SUM 0x1p24f                // the largest sum of a lane's 32 probabilities of a tile that leaves their reference where it is (of a true maximum: 2^5)
+#define CORE_FAR 0x1p23f                // the largest maximum (of products, before their scaling) whose scaled value is a reference good to an eighth of an octave
 
 __device__ __forceinline__ float core_exp2(float x) { return __builtin_amdgcn_exp2f(x); }       // results below 2^-126 are zero
 __device__ __forceinline__ uint32_t core_pk_bf16(float a, float b) {
@@ -139,11 +140,13 @@ struct AttnCore {
     // scores to probabilities 2^(score scale - base) as bf16 pairs, in the order of the registers; their sum, taken before they are rounded (rounded to
     // bf16 a probability is off by at most 2^-8 of itself, as the result is; the sum of the rounded ones, by the pairs' dot product, brought the error at 8192
     // tokens from 0.0022 to 0.0020 of the result, 0.0016 of which is the result's own rounding, for 2 % of the time)
+    // (The maximum is taken off before the scaling here, so that it has weight 1 however large it is; `base` is that to its own rounding.)
     __device__ __forceinline__ float exponentials(const f32x16 (&s)[2], float scale_log2, uint32_t (&p)[16]) const {
+        const float top = m_run == -INFINITY ? 0.f : m_run;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-            const float a = core_exp2(__builtin_fmaf(s[e >> 4][e & 15], scale_log2, -base)), b = core_exp2(__builtin_fmaf(s[e >> 4][(e & 15) + 1], scale_log2, -base));
+            const float a = core_exp2((s[e >> 4][e & 15] - top) * scale_log2), b = core_exp2((s[e >> 4][(e & 15) + 1] - top) * scale_log2);
             sum[0] += a;
             sum[1] += b;
             p[e >> 1] = core_pk_bf16(a, b);
@@ -151,8 +154,9 @@ struct AttnCore {
         return sum[0] + sum[1];
     }
     // The reference `base` need not be the maximum: bf16 and fp32 have one range of exponents, so a probability above 1 loses nothing by itself, and the tile's
-    // maximum is looked for (look) only before a sum passes CORE_SUM, or while there is no maximum: a query whose scores were all -inf has no reference, and what
-    // it summed without one would be dropped with the first that it gets.  (Nothing above 2^-126 of the largest is lost.)
+    // maximum is looked for (look) only before a sum passes CORE_SUM, while there is no maximum (a query whose scores were all -inf has no reference, and what
+    // it summed without one would be dropped with the first that it gets), or where it is so large that the reference's rounding is octaves.  (Nothing above 2^-126
+    // of the largest is lost.)
     // The products with V share that range: n keys have a sum of up to 2^19 n, so values are finite on the way up to max |v| = 2^108 / n (with the true maximum, 2^127 / n).  What the limit
     // costs where scores spread widely, by 1, 3 and 10 nats: 8192 tokens 982, 1002, 1070 us, four trees of 68 rows 54, 52.4, 61; with 2^16 983, 1015, 1097 and 54, 53.3, 66, with 2^6
     // 1004, 1096, 1180 and 55, 63, 70; with 2^60, where values of 2^68 overflowed, 984, 1001, 1006 and 54, 52.5, 53.
@@ -164,7 +168,7 @@ struct AttnCore {
                 take_maximum(largest(s), scale_log2);
             }
             sum = exponentials(s, scale_log2, p);
-            if (look || __builtin_amdgcn_ballot_w64(sum > CORE_SUM || m_run == -INFINITY) == 0) break;
+            if (look || __builtin_amdgcn_ballot_w64(sum > CORE_SUM || !(fabsf(m_run) < CORE_FAR)) == 0) break;
             look = true;
         }
         l_run += sum;
@@ -200,7 +204,7 @@ struct AttnCore {
         });
         __builtin_amdgcn_s_setprio(0);
         float total = sum[0] + sum[1];
-        if (__builtin_amdgcn_ballot_w64(total > CORE_SUM || m_run == -INFINITY) != 0) {
+        if (__builtin_amdgcn_ballot_w64(total > CORE_SUM || !(fabsf(m_run) < CORE_FAR)) != 0) {
             asm volatile("" : "+v"(s[0]), "+v"(s[1]));                          // (else the maximum is taken of every tile, ahead of time)
             take_maximum(largest(s), scale_log2);
             total = exponentials(s, scale_log2, p);
