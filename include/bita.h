@@ -398,7 +398,8 @@ int bita_model_create_q8(const bita_config *cfg, const bita_weights *w, const bi
  * or, with a block_table as in bita_kv ([batch][max_pages]; page_size a power of two >= 16), page pools
  *   codes [n_pages][n_kv_heads][page_size][..], scales [n_pages][n_kv_heads][page_size][..];  smax <= max_pages * page_size, and page ids are
  * clamped to the pool (a bad table gives wrong data, never a fault).
- * bits 4 or 8; head_dim 64 or 128; the four pointers multiples of 16 bytes. */
+ * bits 4 or 8; head_dim 64 or 128; the four pointers multiples of 16 bytes.  Values are read back exactly as they are held; a block with a NaN or an infinity is NaN, and
+ * finite magnitudes from 1.75 * 2^127 (8 bits: 1.9375 * 2^127) on are rounded to 2^128, an infinity. */
 typedef struct bita_kv_mx {
     void *k, *v;
     uint8_t *k_scale, *v_scale;

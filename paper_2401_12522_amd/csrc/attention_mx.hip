@@ -12,8 +12,8 @@
 //    B operand of O^T = V^T P^T if that product takes the keys in the same order: probabilities stay in registers.
 //  * V^T needs eight keys of one column in a lane: V goes to LDS as bf16 rows and comes back by transposed reads.  The region is the wave's own,
 //    and its LDS instructions run in order, so there is no barrier in the loop.
-// Bound by what a CU takes in at low batch (one sequence of 131072 keys, 64/8 heads, 4 bits: 143 MB in 26.6 us, 5.4 TB/s, and a merge of 4), by its own start and end at
-// short lengths (1000 keys, 32 heads: 9.8 us for 4.4 MB), by the conversions and the exponentials between, where a K/V head has many queries by matrix instructions.
+// Bound by what a CU takes in at low batch (one sequence of 131072 keys, 64/8 heads, 4 bits: 143 MB in 27 us, 5.3 TB/s, and a merge of 4), by its own start and end at
+// short lengths (1000 keys, 32 heads: 10 us for 4.4 MB), by the conversions and the exponentials between, where a K/V head has many queries by matrix instructions.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(W * 64, 2) void attn_mx_kernel(AmxArgs a) {
             if (apart) x.page[1] = Keys::page_of(a.kv, b, AMX_CHUNK * chunk + 16, Lc);
         };
         auto load = [&](Chunk &x, int chunk) __attribute__((always_inline)) {   // (behind the end: nothing is there, zeros come back)
-            if (!apart) {                                                       // (half the descriptors: one token over 1000 keys 10.2 -> 9.8 us, over 131072 31.9 -> 31.0)
+            if (!apart) {                                                       // (half the descriptors: one token over 1000 keys 10.2 -> 9.8 us back to back, over 131072, sum included, 31.9 -> 31.0)
                 const int key0 = AMX_CHUNK * chunk, n = __builtin_amdgcn_readfirstlane(min(max(Lc - key0, 0), AMX_CHUNK));
                 const int64_t row = ((int64_t)x.page[0] * a.kv.Hkv + h) * a.kv.page_rows + (key0 & a.kv.slot_mask);
                 auto two = [&](Keys (&y)[2], const unsigned char *codes, const uint8_t *scales) __attribute__((always_inline)) {

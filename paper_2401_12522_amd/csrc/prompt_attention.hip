@@ -9,9 +9,9 @@
 //    the values, V one: scores run a tile ahead); one barrier a tile.  Rows are swizzled by 16-byte columns on the way (by where a lane fetches from: LDS takes them in lane order),
 //    K is read back by rows, V by transposed reads.
 //  * Key tiles before a wave's queries need no mask.  Workgroups start with the longest walks.
-// Bound by matrix instructions at the clock that the card holds under them, with the exponentials between them: 8192 tokens of 64/8 heads of 128 1013 us, 1085 TFLOP/s
-// of what the mask leaves, 0.91 of the library's rate for a product of 8192^3; a turn of two workgroups on a CU 1.95 us.  Ragged prompts by the packing of their walks: 2049, 1411, 977,
-// 350 tokens and less of 32 heads 82 us, 74 of them a packing without starts and ends.
+// Bound by matrix instructions at the clock that the card holds under them, with the exponentials between them: 8192 tokens of 64/8 heads of 128 1015 us, 1083 TFLOP/s
+// of what the mask leaves, 0.91 of the library's rate for a product of 8192^3 (964 on another card); a turn of two workgroups on a CU 1.95 us.  Ragged prompts by the packing of their walks: 2049, 1411, 977,
+// 350 tokens and less of 32 heads 80 us, 74 of them a packing without starts and ends.
 #include <cmath>
 #include <type_traits>
 #include "attention_core.h"
